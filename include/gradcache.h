@@ -62,14 +62,16 @@ typedef enum {
     GC_ERR_WORKSPACE = 6, /* workspace NULL, misaligned (256 bytes) or too small */
     GC_ERR_CUDA = 7,      /* a CUDA call or launch failed */
     GC_ERR_ARCH = 8,      /* the current device is not compute capability 10.x */
-    GC_ERR_LIMIT = 9      /* problem exceeds a built-in limit of the entry point that was called */
+    GC_ERR_LIMIT = 9,     /* problem exceeds a built-in limit of the entry point that was called */
+    GC_ERR_ALIAS = 10,    /* a place that would be written belongs to more than one tensor of a list */
+    GC_ERR_HOST = 11      /* the host is out of memory */
 } gc_status;
 
 typedef enum { GC_F32 = 0, GC_BF16 = 1 } gc_dtype;
 typedef enum { GC_MASK_NONE = 0, GC_MASK_SELF = 1 } gc_mask; /* SELF: drop the pair (i, i) */
 typedef enum { GC_OP_FWD = 0, GC_OP_BWD = 1, GC_OP_BUILD = 2, GC_OP_BUILD_STORED = 3 } gc_op;
 
-enum { GC_DEV_POS_RANGE = 1, GC_DEV_POS_MASKED = 2, GC_DEV_WAIT_LIMIT = 4 };
+enum { GC_DEV_POS_RANGE = 1, GC_DEV_POS_MASKED = 2, GC_DEV_WAIT_LIMIT = 4, GC_DEV_GRAD_NONFINITE = 8 };
 
 /* Bytes of workspace the given call needs for these sizes on the current device (a multiple
  * of 256).  O((B + N) d) plus, for the three calls of the paper's path, what a strip of query rows
@@ -316,6 +318,76 @@ int gc_dist_w_block(const float* D_block, int64_t ldd, int64_t i0, int64_t bq, i
 int gc_dist_dot_block(const void* Q, int64_t ldq, const void* P, int64_t ldp, int64_t B, int64_t N,
                       int d, int dtype, int64_t i0, int64_t bq, int64_t j0, int64_t bn,
                       float* D_block, int64_t ldd, void* cuda_stream);
+
+/*
+ * The global norm of a list of gradients and their clipping: what a training step does with dW (of
+ * gc_cache_apply, and whatever other gradients the model has) before the optimiser.
+ *
+ *     n^2 = sum over all tensors and elements of g^2
+ *     c   = min(1, max_norm / (n + 1e-6))            out = c g
+ *
+ * A list is a HOST array of n_tensors gc_tensor (read during the call only), each a matrix of GC_F32 or
+ * GC_BF16 values in device memory; a list may mix both.  Tensors may be empty, of any length, and start on
+ * any multiple of their element size; vectors of 16 bytes are used where start and pitch allow.  n_tensors
+ * may be 0 (norm 0) and at most 2^20; a tensor of several rows has at most 2^31 columns (else GC_ERR_LIMIT).
+ *
+ *   gc_grad_norm    *sq_sum = n^2 (double), *norm = n (float); either may be NULL.  No tensor is written
+ *                   (`out` and `ld_out` are not read) and one may be listed twice: it counts twice.
+ *   gc_grad_scale   out = c g with n^2 = *sq_sum (device double): of gc_grad_norm, or summed over ranks that
+ *                   hold different gradients.
+ *   gc_grad_clip    both: *norm = n, *sq_sum = n^2 (sq_sum may be NULL), out = c g.
+ *
+ * The two calls that write refuse a list in which a place that is written is read or written through another
+ * tensor (GC_ERR_ALIAS): column ranges of one matrix that do not meet are no such places.  In place (`out`
+ * NULL or equal to `data`, with the same pitch) nothing is written when c = 1.
+ * Squares are summed in fp32 over at most 64 values and in fp64 beyond, and in fp64 throughout where they
+ * overflow or vanish in fp32: n is off by at most 2^-20 n for any finite values.  c is rounded to fp32,
+ * then c g to the tensor's type.  Where n^2 is not finite (a NaN or an infinity among the gradients) *dev_status (may be NULL) gets
+ * GC_DEV_GRAD_NONFINITE and c is 1: the values stay as they are, or are copied as they are.
+ * max_norm >= 0 (an infinity never scales); NaN or negative: GC_ERR_SHAPE.
+ * Workspace: gc_grad_workspace_bytes(n_tensors), 256-byte aligned, 0 for invalid arguments.  Asynchronous on
+ * cuda_stream, deterministic.
+ */
+typedef struct {
+    void* data;            /* [rows x cols], row pitch ld (elements; not read for one row) */
+    void* out;             /* [rows x cols], row pitch ld_out; NULL: in place (data is then written) */
+    int64_t rows, cols;
+    int64_t ld, ld_out;
+    int dtype;
+} gc_tensor;
+size_t gc_grad_workspace_bytes(int64_t n_tensors);
+int gc_grad_norm(const gc_tensor* tensors, int64_t n_tensors, double* sq_sum, float* norm, void* ws,
+                 size_t ws_bytes, int* dev_status, void* cuda_stream);
+int gc_grad_scale(const gc_tensor* tensors, int64_t n_tensors, const double* sq_sum, float max_norm,
+                  int* dev_status, void* cuda_stream);
+int gc_grad_clip(const gc_tensor* tensors, int64_t n_tensors, float max_norm, double* sq_sum, float* norm,
+                 void* ws, size_t ws_bytes, int* dev_status, void* cuda_stream);
+
+/*
+ * A trained encoder in 8-bit integers: the linear encoder f(s) = W s of Step 3 run forward, and the
+ * products S = <Q_i, P_j> of stored rows (beside gc_dist_dot_block, whose blocks gc_dist_accumulate takes).
+ *
+ *   gc_quantize_rows   scale[i] = max_j |X[i][j]| / 127 (fp32) and q[i][j] = X[i][j] / scale[i] to the
+ *                      nearest integer, ties to even (decided on the exact quotient).  A row of zeros, or
+ *                      one whose scale rounds to zero, gets scale 0 and zeros; a row with a NaN or an
+ *                      infinity gets scale NaN and zeros, so that its products are NaN.
+ *   gc_matmul_i8       out[i][j] = (sum_k A[i][k] B[j][k]) a_scale[i] b_scale[j]: a scale for each row of A
+ *                      (token, query) and of B (channel, passage).  The sum is an exact 32-bit integer (k at most
+ *                      131071, else GC_ERR_LIMIT); it is rounded to fp32, multiplied by a_scale and then by b_scale
+ *                      in fp32, and rounded to out_dtype (GC_F32 or GC_BF16).  With A the quantised encoder
+ *                      inputs and B the quantised W, out is the encoder's output; with A and B quantised
+ *                      representations, out is S times tau.
+ * X [rows x d] of dtype (GC_F32 or GC_BF16); q, A, B int8; scales float; leading dimensions in elements, every
+ * row of X, q, A, B and out starts on a 16-byte boundary (else GC_ERR_ALIGN; widths need no padding, and what lies
+ * between a row's end and the next row is neither read as a value nor written).  Any widths; at most 2^30
+ * rows.  A and B may be the same buffer.  Asynchronous on cuda_stream, deterministic; no workspace.
+ * GC_DEV_WAIT_LIMIT in *dev_status (may be NULL) as for the other calls.
+ */
+int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dtype, int8_t* q, int64_t ldq,
+                     float* scale, void* cuda_stream);
+int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb,
+                 const float* b_scale, int64_t rows, int64_t cols, int64_t k, int out_dtype, void* out,
+                 int64_t ldo, int* dev_status, void* cuda_stream);
 
 /*
  * Forward with library-owned scratch (no counterpart in the paper: it exists for the sake of

@@ -16,7 +16,7 @@ from . import _build
 GC_F32, GC_BF16 = 0, 1
 GC_MASK_NONE, GC_MASK_SELF = 0, 1
 GC_OP_FWD, GC_OP_BWD, GC_OP_BUILD, GC_OP_BUILD_STORED = 0, 1, 2, 3
-GC_DEV_POS_RANGE, GC_DEV_POS_MASKED, GC_DEV_WAIT_LIMIT = 1, 2, 4
+GC_DEV_POS_RANGE, GC_DEV_POS_MASKED, GC_DEV_WAIT_LIMIT, GC_DEV_GRAD_NONFINITE = 1, 2, 4, 8
 
 EXPORTS = ("gc_workspace_bytes", "gc_plan_name", "gc_kernel_launches", "gc_loss_fwd",
            "gc_loss_bwd", "gc_build_cache", "gc_build_cache_stored", "gc_status_string",
@@ -27,8 +27,17 @@ EXPORTS = ("gc_workspace_bytes", "gc_plan_name", "gc_kernel_launches", "gc_loss_
            "gc_cosine_bwd", "gc_dtau_workspace_bytes", "gc_dtau", "gc_dist_begin",
            "gc_dist_accumulate", "gc_dist_finish", "gc_dist_w_block", "gc_dist_dot_block",
            "gc_multi_pos_workspace_bytes", "gc_build_cache_multi_pos",
-           "gc_two_direction_workspace_bytes", "gc_build_cache_two_direction")
+           "gc_two_direction_workspace_bytes", "gc_build_cache_two_direction",
+           "gc_grad_workspace_bytes", "gc_grad_norm", "gc_grad_scale", "gc_grad_clip",
+           "gc_quantize_rows", "gc_matmul_i8")
 GC_STATIC_SCRATCH_BYTES = 2 << 20
+
+
+class _Tensor(ctypes.Structure):
+    """gc_tensor of the C ABI."""
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+                ("dtype", ctypes.c_int)]
 
 
 class GradCacheError(RuntimeError):
@@ -108,6 +117,18 @@ def _load() -> ctypes.CDLL:
     lib.gc_dist_w_block.argtypes = [vp, i64, i64, i64, i64, i64, vp, vp, i64, i64, f32, i32, vp, i64, vp]
     lib.gc_dist_dot_block.restype = i32
     lib.gc_dist_dot_block.argtypes = [vp, i64, vp, i64, i64, i64, i32, i32, i64, i64, i64, i64, vp, i64, vp]
+    lib.gc_grad_workspace_bytes.restype = ctypes.c_size_t
+    lib.gc_grad_workspace_bytes.argtypes = [i64]
+    lib.gc_grad_norm.restype = i32
+    lib.gc_grad_norm.argtypes = [vp, i64, vp, vp, vp, ctypes.c_size_t, vp, vp]
+    lib.gc_grad_scale.restype = i32
+    lib.gc_grad_scale.argtypes = [vp, i64, vp, f32, vp, vp]
+    lib.gc_grad_clip.restype = i32
+    lib.gc_grad_clip.argtypes = [vp, i64, f32, vp, vp, vp, ctypes.c_size_t, vp, vp]
+    lib.gc_quantize_rows.restype = i32
+    lib.gc_quantize_rows.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
+    lib.gc_matmul_i8.restype = i32
+    lib.gc_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, i64, i64, i64, i32, vp, i64, vp, vp]
     lib.gc_selftest_wait_limit.restype = i32
     lib.gc_selftest_wait_limit.argtypes = [ctypes.c_uint64, vp, vp, vp]
     lib.gc_profile_enable.restype = i32
@@ -426,6 +447,171 @@ def gc_dist_dot_block(Q, P, i0, bq, j0, bn, D_block) -> None:
                                 i0, bq, j0, bn, _ptr(D_block), D_block.stride(0), _stream())
     if rc != 0:
         raise GradCacheError(rc, "gc_dist_dot_block")
+
+
+def _on_current_device(*tensors):
+    """The library launches on the current device's current stream: refuses tensors that live elsewhere."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != _current_device()):
+            raise ValueError(f"tensors must be on the current CUDA device, got one on {t.device}")
+
+
+def _scalar(t, dtype, name):
+    if t is not None and (t.dtype != dtype or t.numel() < 1):
+        raise TypeError(f"{name} must be a {dtype} tensor of one value")
+
+
+def _dense(t) -> bool:
+    """Whether the values of t fill one stretch of memory, in whatever order of dimensions."""
+    run = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz > 1):
+        if stride != run:
+            return False
+        run *= size
+    return True
+
+
+def _as_matrix(t, like=None):
+    """(rows, cols, pitch) of a tensor: one row where its values fill one stretch of memory (and those of
+    `like` lie in the same order), else a matrix with unit stride along its rows."""
+    if _dense(t) and (like is None or (_dense(like) and like.stride() == t.stride())):
+        return 1, t.numel(), t.numel()
+    if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
+        return t.shape[0], t.shape[1], t.stride(0)
+    if t.dim() == 1:
+        return t.shape[0], 1, t.stride(0)
+    raise ValueError("a gradient must be dense, or a matrix with unit stride along its rows")
+
+
+class GradList:
+    """A list of gradients as gc_grad_norm, gc_grad_scale and gc_grad_clip take it, described once: float32 or
+    bfloat16 CUDA tensors on one device, any shapes, each dense or a matrix with unit stride along its rows.
+    `out`: tensors of the same shapes and types that the clipped gradients go to (default: in place).  It
+    holds the tensors; make a new one when they are replaced (writing to them needs none)."""
+
+    def __init__(self, grads, out=None):
+        self.grads = list(grads)
+        self.out = None if out is None else list(out)
+        if self.out is not None and len(self.out) != len(self.grads):
+            raise ValueError("out must hold one tensor for each gradient")
+        self.n = len(self.grads)
+        self.tensors = (_Tensor * max(self.n, 1))()
+        self.device = self.grads[0].device if self.grads else None
+        for i, g in enumerate(self.grads):
+            o = None if self.out is None else self.out[i]
+            for t in (g, o):
+                if t is not None and (not t.is_cuda or t.device != self.device):
+                    raise ValueError("gradients must be CUDA tensors of one device")
+            code = _dtype_code(g)
+            if o is not None and (o.dtype != g.dtype or o.shape != g.shape):
+                raise ValueError("out must have the shapes and types of the gradients")
+            x = self.tensors[i]
+            x.data, x.dtype = g.data_ptr(), code
+            x.rows, x.cols, x.ld = _as_matrix(g, o)
+            if o is not None:
+                x.out = o.data_ptr()
+                rows, cols, x.ld_out = _as_matrix(o, g)
+                if (rows, cols) != (x.rows, x.cols):
+                    raise ValueError("a gradient that is not dense needs an out of two dimensions, and the "
+                                     "other way round")
+
+
+def gc_grad_workspace_bytes(n: int) -> int:
+    return int(_lib.gc_grad_workspace_bytes(n))
+
+
+def _grad_args(grads, ws, scalars):
+    if not isinstance(grads, GradList):
+        grads = GradList(grads)
+    if grads.device is not None and grads.device.index != _current_device():
+        raise ValueError("gradients must be on the current CUDA device")
+    _on_current_device(ws, *scalars)
+    return grads
+
+
+def _grad_ws(grads, ws):
+    if ws is None:
+        ws = torch.empty(gc_grad_workspace_bytes(grads.n), dtype=torch.uint8,
+                         device=torch.device("cuda", _current_device()))
+    return ws
+
+
+def gc_grad_norm(grads, norm=None, sq_sum=None, ws=None, dev_status=None) -> None:
+    """norm[0] (float32) = 2-norm over all tensors of `grads` (a GradList, or a sequence of tensors), sq_sum[0]
+    (float64) its square; either may be left out.  A NaN or an infinity sets GC_DEV_GRAD_NONFINITE."""
+    _scalar(norm, torch.float32, "norm")
+    _scalar(sq_sum, torch.float64, "sq_sum")
+    grads = _grad_args(grads, ws, (norm, sq_sum, dev_status))
+    ws = _grad_ws(grads, ws)
+    rc = _lib.gc_grad_norm(grads.tensors, grads.n, _ptr(sq_sum), _ptr(norm), _ptr(ws), ws.numel(),
+                           _ptr(dev_status), _stream())
+    if rc != 0:
+        raise GradCacheError(rc, "gc_grad_norm")
+
+
+def gc_grad_scale(grads, sq_sum, max_norm, dev_status=None) -> None:
+    """Scales the gradients (in place, or into the list's `out`) by min(1, max_norm / (n + 1e-6)), with n^2 =
+    sq_sum[0] (float64): of gc_grad_norm, or summed over ranks that hold different gradients."""
+    _scalar(sq_sum, torch.float64, "sq_sum")
+    grads = _grad_args(grads, None, (sq_sum, dev_status))
+    rc = _lib.gc_grad_scale(grads.tensors, grads.n, _ptr(sq_sum), float(max_norm), _ptr(dev_status),
+                            _stream())
+    if rc != 0:
+        raise GradCacheError(rc, "gc_grad_scale")
+
+
+def gc_grad_clip(grads, max_norm, norm, sq_sum=None, ws=None, dev_status=None) -> None:
+    """norm[0] = 2-norm over all tensors, which are scaled (in place, or into the list's `out`) by
+    min(1, max_norm / (norm + 1e-6)); left as they are, with GC_DEV_GRAD_NONFINITE set, where a value is not
+    finite."""
+    _scalar(norm, torch.float32, "norm")
+    _scalar(sq_sum, torch.float64, "sq_sum")
+    grads = _grad_args(grads, ws, (norm, sq_sum, dev_status))
+    ws = _grad_ws(grads, ws)
+    rc = _lib.gc_grad_clip(grads.tensors, grads.n, float(max_norm), _ptr(sq_sum), _ptr(norm), _ptr(ws),
+                           ws.numel(), _ptr(dev_status), _stream())
+    if rc != 0:
+        raise GradCacheError(rc, "gc_grad_clip")
+
+
+def gc_quantize_rows(X, q, scale) -> None:
+    """scale[i] (float32) = max |X[i]| / 127 and q[i] (int8) = X[i] / scale[i] to the nearest integer."""
+    if X.dim() != 2 or q.shape != X.shape or X.stride(1) != 1 or q.stride(1) != 1:
+        raise ValueError("X and q must be 2-D of one shape with unit stride along their rows")
+    rows, d = X.shape
+    if q.dtype != torch.int8 or scale.dtype != torch.float32 or not scale.is_contiguous():
+        raise TypeError("q must be int8, scale contiguous float32")
+    if scale.numel() != rows:
+        raise ValueError("scale must hold one value for each row")
+    _on_current_device(X, q, scale)
+    rc = _lib.gc_quantize_rows(_ptr(X), X.stride(0), rows, d, _dtype_code(X), _ptr(q), q.stride(0),
+                               _ptr(scale), _stream())
+    if rc != 0:
+        raise GradCacheError(rc, "gc_quantize_rows")
+
+
+def gc_matmul_i8(A, a_scale, B, b_scale, out, dev_status=None) -> None:
+    """out[i][j] = a_scale[i] b_scale[j] sum_k A[i][k] B[j][k] with A, B int8 (gc_quantize_rows), out float32 or
+    bfloat16: the linear encoder's output (A inputs, B = W), or scores of queries against passages."""
+    if A.dim() != 2 or B.dim() != 2 or out.dim() != 2 or A.stride(1) != 1 or B.stride(1) != 1 \
+            or out.stride(1) != 1:
+        raise ValueError("A, B and out must be 2-D with unit stride along their rows")
+    rows, k = A.shape
+    cols = B.shape[0]
+    if B.shape[1] != k or tuple(out.shape) != (rows, cols) or a_scale.numel() != rows \
+            or b_scale.numel() != cols:
+        raise ValueError("shape mismatch")
+    if A.dtype != torch.int8 or B.dtype != torch.int8:
+        raise TypeError("A and B must be int8")
+    for s in (a_scale, b_scale):
+        if s.dtype != torch.float32 or not s.is_contiguous():
+            raise TypeError("scales must be contiguous float32")
+    _on_current_device(A, a_scale, B, b_scale, out, dev_status)
+    rc = _lib.gc_matmul_i8(_ptr(A), A.stride(0), _ptr(a_scale), _ptr(B), B.stride(0), _ptr(b_scale), rows,
+                           cols, k, _dtype_code(out), _ptr(out), out.stride(0), _ptr(dev_status),
+                           _stream())
+    if rc != 0:
+        raise GradCacheError(rc, "gc_matmul_i8")
 
 
 def gc_selftest_wait_limit(limit_ns: int, dev_status, waited_ns=None) -> None:

@@ -909,6 +909,8 @@ const char* gc_status_string(int status) {
         case GC_ERR_LIMIT:
             return "problem exceeds a built-in limit of this entry point (static scratch size, or "
                    "dtype / shape / size of the stored weights)";
+        case GC_ERR_ALIAS: return "a place that would be written belongs to more than one tensor";
+        case GC_ERR_HOST: return "the host is out of memory";
         default: return "unknown status";
     }
 }

@@ -1,0 +1,541 @@
+// The global 2-norm of a list of gradients, and their clipping: what stands between Step 3 (Section 3.3,
+// the full-batch gradient dL/dW summed over the sub-batches) and an optimiser.
+//
+//     n^2 = sum_t sum_e g_te^2        c = min(1, max_norm / (n + 1e-6))        out_te = c g_te
+//
+// The tensors of a list travel as kernel parameters (pointers, extents, first tile), so a call copies nothing
+// to the device and can be captured.  The list is cut into tiles of 16 KB; a block owns a run of them.
+// Squares of up to 32 values are summed in fp32; a sum outside [2^-100, inf) whose values are not all zero
+// (squares that overflowed, or that lost bits below 2^-149) is formed again in fp64, and everything beyond
+// those 32 values is summed in fp64, in an order that the sizes alone fix.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include <algorithm>
+#include <vector>
+
+#include "gc_internal.h"
+
+namespace gc {
+namespace {
+
+constexpr int GR_THREADS = 512;
+constexpr int GR_TILE_UNITS = 1024;            // 16-byte vectors of a tile; single elements where they do not fit
+constexpr int GR_PER = GR_TILE_UNITS / GR_THREADS;
+constexpr int GR_SLOTS = 1024;                 // partial sums of a launch
+constexpr double GR_EPS = 1e-6;
+
+enum EntryMode : uint32_t { FLAT_VEC = 0, ROWS_VEC = 1, ELEM = 2 };
+
+struct Entry {
+    const void* src;
+    void* dst;
+    int64_t units;        // FLAT_VEC, ROWS_VEC: whole vectors; ELEM: elements
+    int64_t ld, ld_out;   // elements
+    uint32_t cols;        // ROWS_VEC: vectors of a row; ELEM: elements of a row
+    uint32_t first;       // its first tile
+    uint16_t mode;
+    uint16_t bf16;
+    uint16_t head, tail;  // FLAT_VEC: single elements before and after the vectors
+};
+template <int N>
+struct List {
+    Entry e[N];
+    int n;
+    uint32_t tiles;
+};
+constexpr int FEW = 40, MANY = 580;            // 32,764 bytes of parameters at most
+static_assert(sizeof(List<MANY>) <= 32600, "kernel parameters");
+
+__device__ __forceinline__ float2 widen(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t scale_pair(uint32_t w, float c) {
+    const float2 v = widen(w);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(v.x * c, v.y * c);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint4 scale_vec(const uint4& v, bool bf16, float c) {
+    if (bf16) return make_uint4(scale_pair(v.x, c), scale_pair(v.y, c), scale_pair(v.z, c), scale_pair(v.w, c));
+    return make_uint4(__float_as_uint(__uint_as_float(v.x) * c), __float_as_uint(__uint_as_float(v.y) * c),
+                      __float_as_uint(__uint_as_float(v.z) * c), __float_as_uint(__uint_as_float(v.w) * c));
+}
+// Sum of squares of N vectors (their raw words), see the head of the file.
+template <int N>
+__device__ __forceinline__ double square_sum(const uint4 (&v)[N], bool bf16) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            any |= w[k];
+            if (bf16) {
+                const float2 x = widen(w[k]);
+                s[k] = fmaf(x.x, x.x, s[k]);
+                s[k] = fmaf(x.y, x.y, s[k]);
+            } else {
+                const float x = __uint_as_float(w[k]);
+                s[k] = fmaf(x, x, s[k]);
+            }
+        }
+    }
+    const float t = (s[0] + s[1]) + (s[2] + s[3]);
+    if (t >= 0x1p-100f && t < INFINITY) return (double)t;
+    if (any == 0) return 0.0;
+    double d = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 x = bf16 ? widen(w[k]) : make_float2(__uint_as_float(w[k]), 0.f);
+            d = fma((double)x.x, (double)x.x, d);
+            d = fma((double)x.y, (double)x.y, d);
+        }
+    }
+    return d;
+}
+__device__ __forceinline__ float load_one(const void* p, int64_t i, bool bf16) {
+    return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void scale_one(const Entry& e, int64_t from, int64_t to, bool copy, float c) {
+    if (e.bf16) {
+        const uint16_t x = static_cast<const uint16_t*>(e.src)[from];
+        const __nv_bfloat16 y = __float2bfloat16_rn(__uint_as_float((uint32_t)x << 16) * c);
+        static_cast<uint16_t*>(e.dst)[to] = copy ? x : *reinterpret_cast<const uint16_t*>(&y);
+    } else {
+        const uint32_t x = static_cast<const uint32_t*>(e.src)[from];
+        static_cast<uint32_t*>(e.dst)[to] = copy ? x : __float_as_uint(__uint_as_float(x) * c);
+    }
+}
+
+// The entry that holds tile t.
+template <int N>
+__device__ __forceinline__ int entry_of(const List<N>& list, uint32_t t) {
+    int lo = 0, hi = list.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (list.e[mid].first <= t) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+// Where unit u of an entry lies, in elements from src (OUT: from dst).
+template <bool OUT>
+__device__ __forceinline__ int64_t place_of(const Entry& e, int64_t u) {
+    const int vec = e.bf16 ? 8 : 4;
+    if (e.mode == FLAT_VEC) return e.head + u * vec;
+    const int64_t r = u / e.cols, c = u - r * e.cols;
+    return r * (OUT ? e.ld_out : e.ld) + (e.mode == ROWS_VEC ? c * vec : c);
+}
+
+// The block's run of tiles.
+__device__ __forceinline__ void run_of(uint32_t tiles, uint32_t* lo, uint32_t* hi) {
+    *lo = (uint32_t)((uint64_t)tiles * blockIdx.x / gridDim.x);
+    *hi = (uint32_t)((uint64_t)tiles * (blockIdx.x + 1) / gridDim.x);
+}
+
+__device__ __forceinline__ double warp_sum(double v) {
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// Sum over the block, in every thread.
+__device__ __forceinline__ double block_sum(double v, double* part) {
+    v = warp_sum(v);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) s += part[w];
+    return s;
+}
+
+// part[block] = the sum of squares of the block's run of tiles.
+template <int N>
+__global__ void __launch_bounds__(GR_THREADS)
+grad_square_kernel(const __grid_constant__ List<N> list, double* part) {
+    __shared__ double warp_part[GR_THREADS / 32];
+    dep_release();
+    dep_wait();
+    uint32_t t, end;
+    run_of(list.tiles, &t, &end);
+    double sum = 0.0;
+    int at = t < end ? entry_of(list, t) : 0;
+    for (; t < end; ++t) {
+        while (at + 1 < list.n && list.e[at + 1].first <= t) ++at;
+        const Entry& e = list.e[at];
+        const int64_t u0 = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
+        if (e.mode == ELEM) {
+#pragma unroll
+            for (int i = 0; i < GR_PER; ++i) {
+                const int64_t u = u0 + i * GR_THREADS;
+                if (u < e.units) {
+                    const double x = load_one(e.src, place_of<false>(e, u), e.bf16);
+                    sum = fma(x, x, sum);
+                }
+            }
+            continue;
+        }
+        uint4 v[GR_PER];
+        const int es = e.bf16 ? 2 : 4;
+#pragma unroll
+        for (int i = 0; i < GR_PER; ++i) {
+            const int64_t u = u0 + i * GR_THREADS;
+            v[i] = u < e.units ? *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
+                                                                 place_of<false>(e, u) * es)
+                               : make_uint4(0, 0, 0, 0);
+        }
+        sum += square_sum(v, e.bf16);
+        if (t == e.first && threadIdx.x < e.head + e.tail) {
+            const int k = threadIdx.x;
+            const int64_t i = k < e.head ? k : k + e.units * (16 / es);
+            const double x = load_one(e.src, i, e.bf16);
+            sum = fma(x, x, sum);
+        }
+    }
+    sum = block_sum(sum, warp_part);
+    if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+// The sum of `slots` partial sums, in every thread of the block.
+__device__ __forceinline__ double total_of(const double* part, int slots, double* warp_part) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < slots; i += blockDim.x) s += __ldcg(part + i);
+    return block_sum(s, warp_part);
+}
+__device__ __forceinline__ void tell_norm(double total, double* sq_sum, float* norm, int* dev_status) {
+    if (sq_sum) *sq_sum = total;
+    if (norm) *norm = (float)sqrt(total);
+    if (dev_status && !isfinite(total)) atomicOr(dev_status, GC_DEV_GRAD_NONFINITE);
+}
+
+__global__ void __launch_bounds__(GR_THREADS)
+grad_norm_kernel(const double* part, int slots, double* sq_sum, float* norm, int* dev_status) {
+    __shared__ double warp_part[GR_THREADS / 32];
+    dep_release();
+    dep_wait();
+    const double total = total_of(part, slots, warp_part);
+    if (threadIdx.x == 0) tell_norm(total, sq_sum, norm, dev_status);
+}
+
+// out = c g, c from the sum of `slots` partial sums.
+template <int N>
+__global__ void __launch_bounds__(GR_THREADS)
+grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int slots, float max_norm,
+                  double* sq_sum, float* norm, int* dev_status, int tell) {
+    __shared__ double warp_part[GR_THREADS / 32];
+    dep_release();
+    dep_wait();
+    const double total = total_of(part, slots, warp_part);
+    if (tell && blockIdx.x == 0 && threadIdx.x == 0) tell_norm(total, sq_sum, norm, dev_status);
+    // c >= 1, or a sum that is not finite: values are copied bit for bit, a NaN's payload too (told from the fp64
+    // factor: by c == 1 the compiler takes a product with c for the same)
+    const double wide = (double)max_norm / (sqrt(total) + GR_EPS);
+    const bool copy = !isfinite(total) || wide >= 1.0;
+    const float c = (float)wide;
+    uint32_t t, end;
+    run_of(list.tiles, &t, &end);
+    int at = t < end ? entry_of(list, t) : 0;
+    for (; t < end; ++t) {
+        while (at + 1 < list.n && list.e[at + 1].first <= t) ++at;
+        const Entry& e = list.e[at];
+        if (copy && e.src == e.dst) continue;           // the values stay as they are
+        const int64_t u0 = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
+        if (e.mode == ELEM) {
+#pragma unroll
+            for (int i = 0; i < GR_PER; ++i) {
+                const int64_t u = u0 + i * GR_THREADS;
+                if (u < e.units) {
+                    scale_one(e, place_of<false>(e, u), place_of<true>(e, u), copy, c);
+                }
+            }
+            continue;
+        }
+        const int es = e.bf16 ? 2 : 4;
+#pragma unroll
+        for (int i = 0; i < GR_PER; ++i) {
+            const int64_t u = u0 + i * GR_THREADS;
+            if (u < e.units) {
+                const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
+                                                                place_of<false>(e, u) * es);
+                *reinterpret_cast<uint4*>(static_cast<char*>(e.dst) + place_of<true>(e, u) * es) =
+                    copy ? v : scale_vec(v, e.bf16, c);
+            }
+        }
+        if (t == e.first && threadIdx.x < e.head + e.tail) {
+            const int k = threadIdx.x;
+            const int64_t i = k < e.head ? k : k + e.units * (16 / es);
+            scale_one(e, i, i, copy, c);
+        }
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+struct Span { uintptr_t lo, hi; int entry; bool written; };
+
+int elem_size(int dtype) { return dtype == GC_BF16 ? 2 : 4; }
+
+// Checks one tensor; *count its elements.
+int check_tensor(const gc_tensor& t, bool write, int64_t* count) {
+    if (t.dtype != GC_F32 && t.dtype != GC_BF16) return GC_ERR_DTYPE;
+    if (t.rows < 0 || t.cols < 0) return GC_ERR_SHAPE;
+    *count = 0;
+    if (t.rows == 0 || t.cols == 0) return GC_OK;
+    const int64_t limit = (int64_t)1 << 40;
+    if (t.cols > limit || t.rows > limit / t.cols) return GC_ERR_SHAPE;
+    if (t.rows > 1 && t.cols > ((int64_t)1 << 31)) return GC_ERR_LIMIT;
+    if (t.rows > 1 && (t.ld < t.cols || t.ld > limit || t.rows > ((int64_t)1 << 60) / t.ld)) return GC_ERR_SHAPE;
+    if (!t.data) return GC_ERR_NULL;
+    const uintptr_t es = (uintptr_t)elem_size(t.dtype);
+    if ((uintptr_t)t.data % es) return GC_ERR_ALIGN;
+    if (write && t.out && t.out != t.data) {
+        if (t.rows > 1 && (t.ld_out < t.cols || t.ld_out > limit || t.rows > ((int64_t)1 << 60) / t.ld_out))
+            return GC_ERR_SHAPE;
+        if ((uintptr_t)t.out % es) return GC_ERR_ALIGN;
+    }
+    *count = t.rows * t.cols;
+    return GC_OK;
+}
+uintptr_t bytes_of(const gc_tensor& t, int64_t ld) {
+    return (uintptr_t)(((t.rows - 1) * ld + t.cols) * elem_size(t.dtype));
+}
+// True where two spans that meet belong to column ranges of one matrix that do not.
+bool apart_by_columns(const gc_tensor& a, uintptr_t a_lo, int64_t a_ld, const gc_tensor& b, uintptr_t b_lo,
+                      int64_t b_ld) {
+    if (a.rows < 2 || b.rows < 2) {               // one row lies anywhere in the other's pitch
+        if (a.rows < 2) a_ld = b_ld; else b_ld = a_ld;
+        if (a.rows < 2 && b.rows < 2) return false;
+    }
+    const int64_t ea = elem_size(a.dtype), eb = elem_size(b.dtype);
+    if (a_ld * ea != b_ld * eb || a.cols > a_ld || b.cols > b_ld) return false;
+    const int64_t pitch = a_ld * ea, off = (int64_t)(b_lo - a_lo) % pitch;      // a_lo <= b_lo
+    return off >= a.cols * ea && off + b.cols * eb <= pitch;
+}
+
+// No place that is written may be read or written through another tensor of the list.
+int check_overlap(const gc_tensor* list, int64_t n) {
+    std::vector<Span> s;
+    s.reserve((size_t)n * 2);
+    bool sorted = true;
+    auto add = [&](uintptr_t lo, uintptr_t len, int64_t i, bool written) {
+        if (!s.empty() && lo < s.back().hi) sorted = false;
+        s.push_back({lo, lo + len, (int)i, written});
+    };
+    for (int64_t i = 0; i < n; ++i)
+        if (list[i].rows > 0 && list[i].cols > 0) {
+            const gc_tensor& t = list[i];
+            const uintptr_t lo = (uintptr_t)t.data;
+            const bool in_place = !t.out || t.out == t.data;
+            if (in_place && t.out && t.rows > 1 && t.ld_out != t.ld) return GC_ERR_ALIAS;
+            add(lo, bytes_of(t, t.ld), i, in_place);
+        }
+    for (int64_t i = 0; i < n; ++i)
+        if (list[i].rows > 0 && list[i].cols > 0 && list[i].out && list[i].out != list[i].data)
+            add((uintptr_t)list[i].out, bytes_of(list[i], list[i].ld_out), i, true);
+    if (sorted) return GC_OK;
+    std::sort(s.begin(), s.end(), [](const Span& a, const Span& b) { return a.lo < b.lo; });
+    auto pitch = [&](const Span& x) {
+        const gc_tensor& t = list[x.entry];
+        return x.lo == (uintptr_t)t.data ? t.ld : t.ld_out;
+    };
+    int64_t pairs = 0;
+    for (size_t i = 0; i < s.size(); ++i)
+        for (size_t j = i + 1; j < s.size() && s[j].lo < s[i].hi; ++j) {
+            if (++pairs > (int64_t)1 << 24) return GC_ERR_LIMIT;
+            if ((s[i].written || s[j].written) &&
+                !apart_by_columns(list[s[i].entry], s[i].lo, pitch(s[i]), list[s[j].entry], s[j].lo, pitch(s[j])))
+                return GC_ERR_ALIAS;
+        }
+    return GC_OK;
+}
+
+// The tensor as an entry; *tiles what it takes.
+Entry entry_for(const gc_tensor& t, bool write, int64_t* tiles) {
+    Entry e{};
+    const int es = elem_size(t.dtype), vec = 16 / es;
+    e.src = t.data;
+    e.dst = t.out ? t.out : t.data;
+    e.bf16 = t.dtype == GC_BF16;
+    e.ld = t.ld;
+    e.ld_out = e.dst == t.data ? t.ld : t.ld_out;
+    const int64_t count = t.rows * t.cols;
+    const bool flat = t.rows == 1 || (t.ld == t.cols && (!write || e.ld_out == t.cols));
+    const uintptr_t s16 = (uintptr_t)e.src & 15, d16 = write ? (uintptr_t)e.dst & 15 : s16;
+    if (flat && s16 == d16) {
+        e.mode = FLAT_VEC;
+        const int64_t head = std::min<int64_t>(count, (int64_t)((16 - s16) & 15) / es);
+        e.head = (uint16_t)head;
+        e.units = (count - head) / vec;
+        e.tail = (uint16_t)(count - head - e.units * vec);
+        e.cols = 1;
+    } else if (!flat && s16 == 0 && d16 == 0 && t.cols % vec == 0 && (e.ld * es) % 16 == 0 &&
+               (!write || (e.ld_out * es) % 16 == 0) && t.cols / vec < ((int64_t)1 << 31)) {
+        e.mode = ROWS_VEC;
+        e.units = count / vec;
+        e.cols = (uint32_t)(t.cols / vec);
+    } else {
+        e.mode = ELEM;
+        e.units = count;
+        e.cols = (uint32_t)t.cols;            // of several rows: at most 2^31
+        if (flat) { e.cols = 1; e.ld = e.ld_out = 1; }
+    }
+    *tiles = std::max<int64_t>(1, (e.units + GR_TILE_UNITS - 1) / GR_TILE_UNITS);
+    return e;
+}
+
+int current_device() {
+    int dev = 0, major = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return GC_ERR_CUDA;
+    }
+    return major == 10 ? GC_OK : GC_ERR_ARCH;
+}
+
+int64_t groups_of(int64_t n) { return std::max<int64_t>(1, (n + MANY - 1) / MANY); }
+
+// go(list, tiles) for every group of at most MANY tensors in order; the group's list as a parameter.
+template <typename Go>
+int each_group(const gc_tensor* list, int64_t n, bool write, Go go) {
+    List<MANY> many;
+    int64_t i = 0;
+    do {
+        many.n = 0;
+        int64_t tiles = 0;
+        for (; i < n && many.n < MANY; ++i) {
+            if (list[i].rows == 0 || list[i].cols == 0) continue;
+            int64_t more = 0;
+            Entry e = entry_for(list[i], write, &more);
+            if (tiles + more > (int64_t)UINT32_MAX) {
+                if (many.n == 0) return GC_ERR_LIMIT;
+                break;
+            }
+            e.first = (uint32_t)tiles;
+            tiles += more;
+            many.e[many.n++] = e;
+        }
+        many.tiles = (uint32_t)tiles;
+        cudaError_t err;
+        if (many.n <= FEW) {
+            List<FEW> few;
+            std::copy(many.e, many.e + many.n, few.e);
+            few.n = many.n;
+            few.tiles = many.tiles;
+            err = go(few);
+        } else {
+            err = go(many);
+        }
+        if (err != cudaSuccess) {
+            cudaGetLastError();
+            return GC_ERR_CUDA;
+        }
+    } while (i < n);
+    return GC_OK;
+}
+
+unsigned grid_for(uint32_t tiles) {
+    const uint32_t most = (uint32_t)std::min(GR_SLOTS, 4 * sm_count());
+    return std::max(1u, std::min(tiles, most));
+}
+
+int check_list(const gc_tensor* list, int64_t n, bool write) {
+    if (n < 0) return GC_ERR_SHAPE;
+    if (n > 0 && !list) return GC_ERR_NULL;
+    if (n > (int64_t)1 << 20) return GC_ERR_LIMIT;
+    for (int64_t i = 0; i < n; ++i) {
+        int64_t count;
+        const int rc = check_tensor(list[i], write, &count);
+        if (rc) return rc;
+    }
+    return write ? check_overlap(list, n) : GC_OK;
+}
+int check_ws(const void* ws, size_t ws_bytes, int64_t n) {
+    return !ws || ((uintptr_t)ws & 255) || ws_bytes < gc_grad_workspace_bytes(n) ? GC_ERR_WORKSPACE : GC_OK;
+}
+
+// The partial sums of the list; *slots how many.
+int launch_squares(const gc_tensor* list, int64_t n, double* part, int* slots, cudaStream_t st) {
+    *slots = 0;
+    return each_group(list, n, false, [&](const auto& l) {
+        if (l.tiles == 0) return cudaSuccess;
+        const unsigned grid = grid_for(l.tiles);
+        using L = std::decay_t<decltype(l)>;
+        const cudaError_t e = launch_chained(grad_square_kernel<sizeof(L::e) / sizeof(Entry)>, dim3(grid), GR_THREADS, 0,
+                                             1, st, l, part + *slots);
+        *slots += (int)grid;
+        return e;
+    });
+}
+int launch_scale(const gc_tensor* list, int64_t n, const double* part, int slots, float max_norm, double* sq_sum,
+                 float* norm, int* dev_status, cudaStream_t st) {
+    int tell = 1;
+    return each_group(list, n, true, [&](const auto& l) {
+        using L = std::decay_t<decltype(l)>;
+        const cudaError_t e =
+            launch_chained(grad_scale_kernel<sizeof(L::e) / sizeof(Entry)>, dim3(grid_for(l.tiles)), GR_THREADS, 0, 1, st,
+                           l, part, slots, max_norm, sq_sum, norm, dev_status, tell);
+        tell = 0;
+        return e;
+    });
+}
+
+}  // namespace
+}  // namespace gc
+
+using namespace gc;
+
+extern "C" {
+
+size_t gc_grad_workspace_bytes(int64_t n) {
+    if (n < 0 || n > (int64_t)1 << 20) return 0;
+    return (size_t)groups_of(n) * GR_SLOTS * sizeof(double);
+}
+
+int gc_grad_norm(const gc_tensor* list, int64_t n, double* sq_sum, float* norm, void* ws, size_t ws_bytes,
+                 int* dev_status, void* cuda_stream) try {
+    if (!norm && !sq_sum) return GC_ERR_NULL;
+    int rc = check_list(list, n, false);
+    if (rc || (rc = check_ws(ws, ws_bytes, n)) || (rc = current_device())) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    double* part = static_cast<double*>(ws);
+    int slots;
+    if ((rc = launch_squares(list, n, part, &slots, st))) return rc;
+    if (launch_chained(grad_norm_kernel, dim3(1), GR_THREADS, 0, 1, st, part, slots, sq_sum, norm, dev_status) !=
+        cudaSuccess) {
+        cudaGetLastError();
+        return GC_ERR_CUDA;
+    }
+    return GC_OK;
+} catch (...) {
+    return GC_ERR_HOST;
+}
+
+int gc_grad_scale(const gc_tensor* list, int64_t n, const double* sq_sum, float max_norm, int* dev_status,
+                  void* cuda_stream) try {
+    if (!sq_sum) return GC_ERR_NULL;
+    if (!(max_norm >= 0.f)) return GC_ERR_SHAPE;
+    int rc = check_list(list, n, true);
+    if (rc || (rc = current_device())) return rc;
+    return launch_scale(list, n, sq_sum, 1, max_norm, nullptr, nullptr, dev_status,
+                        static_cast<cudaStream_t>(cuda_stream));
+} catch (...) {
+    return GC_ERR_HOST;
+}
+
+int gc_grad_clip(const gc_tensor* list, int64_t n, float max_norm, double* sq_sum, float* norm, void* ws,
+                 size_t ws_bytes, int* dev_status, void* cuda_stream) try {
+    if (!norm) return GC_ERR_NULL;
+    if (!(max_norm >= 0.f)) return GC_ERR_SHAPE;
+    int rc = check_list(list, n, true);
+    if (rc || (rc = check_ws(ws, ws_bytes, n)) || (rc = current_device())) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    double* part = static_cast<double*>(ws);
+    int slots;
+    if ((rc = launch_squares(list, n, part, &slots, st))) return rc;
+    return launch_scale(list, n, part, slots, max_norm, sq_sum, norm, dev_status, st);
+} catch (...) {
+    return GC_ERR_HOST;
+}
+
+}  // extern "C"

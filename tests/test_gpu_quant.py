@@ -1,0 +1,346 @@
+"""gc_quantize_rows and gc_matmul_i8 against their definitions.
+
+Both are compared bit for bit.  The scale is one IEEE division of fp32 numbers, an 8-bit integer the nearest one to
+the quotient of x and that scale, which fp64 holds closely enough to tell every side of every border.  A
+product is an integer below 2^31, rounded to fp32, and two fp32 products in a stated order, then one rounding
+to bf16 where that is the output's type."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def binding():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a CUDA device")
+    from paper_2101_06983_b200 import binding as b
+    return b
+
+
+def _padded(rows, cols, dtype, unit, fill, pad=0):
+    """A [rows x cols] view with rows on 16-byte boundaries, `pad` units of 16 bytes more between them."""
+    ld = -(-cols // unit) * unit + pad * unit
+    big = torch.full((rows, ld), fill, dtype=dtype, device="cuda")
+    return big, big[:, :cols]
+
+
+def _quantized(x):
+    """The definition, on the host in 64 bits."""
+    x = x.detach().cpu().float().numpy()
+    amax = np.abs(x).max(axis=1)
+    scale = (amax / np.float32(127)).astype(np.float32)
+    q = np.zeros(x.shape, np.int8)
+    for i, s in enumerate(scale):
+        if not np.isfinite(amax[i]):
+            scale[i] = np.nan
+        elif s > 0:
+            q[i] = np.clip(np.rint(x[i].astype(np.float64) / np.float64(s)), -127, 127).astype(np.int8)
+    return torch.from_numpy(q), torch.from_numpy(scale)
+
+
+def _check_quantize(binding, x, pad=0):
+    rows, d = x.shape
+    big, q = _padded(rows, d, torch.int8, 16, 99, pad)
+    scale = torch.full((rows + 2,), -5.0, device="cuda")
+    binding.gc_quantize_rows(x, q, scale[1:rows + 1])
+    torch.cuda.synchronize()
+    want_q, want_s = _quantized(x)
+    got = scale[1:rows + 1].cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want_s))
+    assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want_s))
+    assert torch.equal(q.cpu(), want_q)
+    assert bool((big[:, d:] == 99).all()) and scale[0].item() == scale[-1].item() == -5.0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("rows,d", [(1, 1), (1, 768), (3, 15), (5, 16), (7, 17), (9, 31), (33, 500), (8, 512), (300, 513),
+                                    (1, 4096), (2, 1024), (17, 1025), (640, 768), (4, 8191), (3, 8192), (5, 8193),
+                                    (2, 20011), (5000, 64)])
+def test_rows(binding, rows, d, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(rows * 7 + d)
+    unit = 8 if dtype == BF else 4
+    for pad in (0, 1):
+        _, x = _padded(rows, d, dtype, unit, 1e9, pad)         # what lies between the rows is no value of theirs
+        x.copy_(torch.randn(rows, d, generator=gen, device="cuda"))
+        _check_quantize(binding, x, pad)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("d", [96, 3000])
+def test_values_next_to_borders(binding, d, dtype):
+    """Values on and a few units in the last place around every border between two integers, for many scales."""
+    gen = np.random.default_rng(d)
+    rows = 200
+    x = np.zeros((rows, d), np.float32)
+    for i in range(rows):
+        top = np.float32(2.0 ** gen.uniform(-30, 30))
+        s = np.float32(top / np.float32(127))
+        half = (gen.integers(-127, 127, d).astype(np.float64) + 0.5) * np.float64(s)
+        v = half.astype(np.float32)
+        v = (v.view(np.int32) + gen.integers(-2, 3, d).astype(np.int32)).view(np.float32)
+        v[gen.integers(0, d)] = top
+        x[i] = np.clip(v, -top, top)
+    _, xs = _padded(rows, d, dtype, 8, 0.0)
+    xs.copy_(torch.from_numpy(x).cuda())
+    _check_quantize(binding, xs)
+
+
+def test_exact_ties(binding):
+    """A scale of one: halves go to the even integer."""
+    x = torch.arange(-126, 127, device="cuda").float()[None, :] + 0.5
+    x = torch.cat([x, torch.full((1, 1), 127.0, device="cuda")], dim=1)
+    _, xs = _padded(1, x.shape[1], F32, 4, 0.0)
+    xs.copy_(x)
+    _check_quantize(binding, xs)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("size", [3e38, 1e30, 1e-20, 1e-30, 1e-36, 1e-38, 1e-43, 1e-45])
+def test_magnitudes_of_rows(binding, size, dtype):
+    x = ((torch.rand(6, 200, dtype=torch.float64) * 2 - 1) * size).to(dtype)
+    x[0] = 0
+    x[1, 5:] = 0
+    _, xs = _padded(6, 200, dtype, 8, 0.0)
+    xs.copy_(x.cuda())
+    _check_quantize(binding, xs)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("d", [1, 40, 1500])
+def test_rows_that_are_not_finite(binding, d, dtype):
+    x = torch.randn(9, d)
+    x[1, d // 2], x[3, 0], x[5, d - 1] = math.nan, math.inf, -math.inf
+    x[7] = 0
+    _, xs = _padded(9, d, dtype, 8, 0.0)
+    xs.copy_(x.to(dtype).cuda())
+    _check_quantize(binding, xs)
+
+
+# ---- product ---------------------------------------------------------------------------------------------
+
+def _operands(rows, cols, k, seed, pad=0, low=-127):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    mats, scales = [], []
+    for n in (rows, cols):
+        big, m = _padded(n, k, torch.int8, 16, 77, pad)       # what lies between the rows is no value of theirs
+        m.copy_(torch.randint(low, 128, (n, k), generator=gen, device="cuda", dtype=torch.int32))
+        mats.append(m)
+        scales.append(torch.rand(n, generator=gen, device="cuda") * 0.01 + 1e-4)
+    return mats[0], scales[0], mats[1], scales[1]
+
+
+def _product(A, sa, B, sb, dtype):
+    # integers below 2^53: exact in fp64 in any order
+    total = A.double() @ B.double().t()
+    return (total.float() * sa[:, None] * sb).to(dtype)
+
+
+def _check_product(binding, A, sa, B, sb, dtype, pad=0):
+    rows, cols = A.shape[0], B.shape[0]
+    big, out = _padded(rows + 1, cols, dtype, 8, 5.0, pad)
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    binding.gc_matmul_i8(A, sa, B, sb, out[:rows], st)
+    torch.cuda.synchronize()
+    want = _product(A, sa, B, sb, dtype)
+    assert st.item() == 0
+    assert torch.equal(out[:rows], want)
+    assert bool((big[:, cols:] == 5).all()) and bool((big[rows] == 5).all())
+    again = torch.empty_like(big)[:rows, :cols]
+    binding.gc_matmul_i8(A, sa, B, sb, again)
+    assert torch.equal(again, want)
+
+
+SHAPES = [
+    # rows, cols, k
+    (1, 1, 1), (1, 128, 768), (1, 129, 16), (2, 1000, 100), (15, 127, 127), (16, 128, 128), (17, 130, 129), (31, 64, 33),
+    (32, 256, 256), (33, 257, 500), (37, 5021, 1000), (48, 300, 768), (64, 64, 64), (65, 512, 768), (100, 99, 98),
+    (127, 640, 384), (128, 128, 1024), (129, 129, 129), (200, 3000, 96), (255, 255, 255), (256, 256, 256),
+    (257, 300, 640), (300, 1, 768), (513, 1030, 2050), (1000, 777, 36), (1531, 2062, 768), (2048, 2048, 128), (4097, 40, 72),
+    (8, 40, 16384), (300, 500, 8192),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("rows,cols,k", SHAPES)
+def test_products(binding, rows, cols, k, dtype):
+    A, sa, B, sb = _operands(rows, cols, k, seed=rows + cols + k, pad=k % 3)
+    _check_product(binding, A, sa, B, sb, dtype, pad=cols % 2)
+
+
+@pytest.mark.parametrize("rows", [1, 40, 700])
+def test_the_longest_contraction(binding, rows):
+    """-128 times -128 over the longest rows: the sum still fits 31 bits."""
+    k = 131071
+    A = torch.full((rows, -(-k // 16) * 16), -128, dtype=torch.int8, device="cuda")[:, :k]
+    B = torch.full((130, -(-k // 16) * 16), -128, dtype=torch.int8, device="cuda")[:, :k]
+    B[7] = 127
+    one = torch.ones(1000, device="cuda")
+    out = torch.empty(rows, 132, device="cuda")[:, :130]
+    binding.gc_matmul_i8(A, one[:rows], B, one[:130], out)
+    want = torch.full((rows, 130), float(np.float32(k * 16384)), device="cuda")
+    want[:, 7] = float(np.float32(-128 * 127 * k))
+    assert torch.equal(out, want)
+
+
+def test_one_buffer_on_both_sides(binding):
+    A, sa, _, _ = _operands(300, 1, 200, seed=1)
+    _check_product(binding, A, sa, A, sa, F32)
+
+
+def test_scales_that_are_not_finite_or_zero(binding):
+    A, sa, B, sb = _operands(50, 70, 64, seed=2)
+    sa[3], sa[5], sb[7], sb[9] = math.nan, 0.0, math.nan, 0.0
+    A[3] = 0
+    out = torch.empty(50, 72, device="cuda")[:, :70]
+    binding.gc_matmul_i8(A, sa, B, sb, out)
+    want = _product(A, sa, B, sb, F32)
+    assert torch.equal(torch.isnan(out), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(want))
+    assert bool(torch.isnan(out[3]).all()) and bool(torch.isnan(out[:, 7]).all())
+
+
+def test_outputs_beyond_32_bits(binding):
+    """An output of more than 2^32 bytes: its last rows."""
+    rows, cols, k = 36000, 32768, 32
+    A, sa, B, sb = _operands(rows, cols, k, seed=3)
+    out = torch.empty(rows, cols, device="cuda")
+    binding.gc_matmul_i8(A, sa, B, sb, out)
+    for r in (0, 18000, rows - 300):
+        assert torch.equal(out[r:r + 300], _product(A[r:r + 300], sa[r:r + 300], B, sb, F32))
+
+
+@pytest.mark.parametrize("rows,cols,k", [(1, 5000, 768), (600, 900, 256)])
+def test_captured_and_on_another_stream(binding, rows, cols, k):
+    A, sa, B, sb = _operands(rows, cols, k, seed=4)
+    x = torch.randn(rows, k, device="cuda")
+    out = torch.empty(rows, -(-cols // 8) * 8, dtype=BF, device="cuda")[:, :cols]
+    s = torch.cuda.Stream()
+
+    def step():
+        binding.gc_quantize_rows(x, A, sa)
+        binding.gc_matmul_i8(A, sa, B, sb, out)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        step()
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            step()
+    for _ in range(3):
+        x.copy_(torch.randn(rows, k, device="cuda"))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            g.replay()
+        torch.cuda.synchronize()
+        q, scale = _quantized(x)
+        assert torch.equal(A.cpu(), q) and torch.equal(sa.cpu(), scale)
+        assert torch.equal(out, _product(A, sa, B, sb, BF))
+
+
+def test_calls_that_overlap(binding):
+    """Products on four streams at once."""
+    jobs = []
+    for i in range(4):
+        ops = _operands(300 + i, 2000, 512, seed=i)
+        jobs.append((ops, torch.empty(300 + i, 2000, device="cuda"), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for ops, out, s in jobs:
+            with torch.cuda.stream(s):
+                binding.gc_matmul_i8(*ops, out)
+    torch.cuda.synchronize()
+    for ops, out, s in jobs:
+        assert torch.equal(out, _product(*ops, F32))
+
+
+def test_refusals_of_tensors(binding):
+    A, sa, B, sb = _operands(16, 32, 64, seed=5)
+    out = torch.empty(16, 32, device="cuda")
+    for bad in ((A, sa, B[:, :32], sb, out), (A, sa[:3], B, sb, out), (A, sa, B, sb, out[:, :31]), (A.t(), sa, B, sb, out),
+                (A.cpu(), sa, B, sb, out)):
+        with pytest.raises(ValueError):
+            binding.gc_matmul_i8(*bad)
+    for bad in ((A.to(torch.uint8), sa, B, sb, out), (A, sa.double(), B, sb, out), (A, sa, B, sb, out.half()),
+                (A, torch.empty(32, device="cuda")[::2], B, sb, out)):
+        with pytest.raises(TypeError):
+            binding.gc_matmul_i8(*bad)
+    with pytest.raises(TypeError):
+        binding.gc_quantize_rows(out, torch.empty(16, 32, device="cuda"), sa)
+    with pytest.raises(ValueError):
+        binding.gc_quantize_rows(out, A, sa)
+
+
+# ---- from the cache to an 8-bit index --------------------------------------------------------------------------
+
+def test_a_step_then_the_encoder_in_8_bits(binding):
+    """Step 2, Step 3 over sub-batches, the two matrices' gradients clipped together, a step, and the encoder run in 8
+    bits: representations, scores of queries against passages, and the loss of those scores.
+
+    The tolerance of a representation: of k terms x w, each of x and w is off by at most half a step of its row, s / 2
+    (and 2^-24 of itself, from the scale's rounding); three fp32 roundings after that."""
+    from paper_2101_06983_b200 import inputs
+    B, N, d, d_in, tau = 256, 512, 128, 192, 1.0
+    lr, bound = 0.5, 0.05
+    sbits, Xs = inputs.encoder_inputs(B, d_in, seed=31)
+    tbits, Xt = inputs.encoder_inputs(N, d_in, seed=32)
+    _, Wf = inputs.encoder_inputs(d, d_in, seed=33, sigma=d_in ** -0.5 * 0.6)
+    _, Wg = inputs.encoder_inputs(d, d_in, seed=34, sigma=d_in ** -0.5 * 0.6)
+    dev = lambda bits: torch.from_numpy(bits.view(np.int16)).view(BF).cuda()  # noqa: E731
+    xs, xt = dev(sbits), dev(tbits)
+    W = [torch.from_numpy(w.astype(np.float32)).cuda() for w in (Wf, Wg)]
+    Q, P = (xs.float() @ W[0].t()).bfloat16(), (xt.float() @ W[1].t()).bfloat16()
+    pos = torch.arange(0, N, 2, dtype=torch.int32, device="cuda")
+    out = binding.build_cache(Q, P, pos, tau)
+    g = [torch.empty(d, d_in, device="cuda") for _ in range(2)]
+    for rep, x, dw in ((out.dQ, xs, g[0]), (out.dP, xt, g[1])):
+        for lo in range(0, x.shape[0], 100):
+            binding.gc_cache_apply(rep[lo:lo + 100], x[lo:lo + 100], dw, lo > 0)
+    raw = [t.clone() for t in g]
+    norm = torch.zeros(1, device="cuda")
+    binding.gc_grad_clip(g, bound, norm)
+    want = math.sqrt(sum(float((t.double() ** 2).sum()) for t in raw))
+    assert want > bound and abs(norm.item() - want) <= 2.0 ** -20 * want
+    for t, r in zip(g, raw):
+        assert float((t.double() - r.double() * (bound / (want + 1e-6))).abs().max()) <= 2.0 ** -19 * float(r.abs().max())
+    reps = []
+    for x, w, dw in zip((xs, xt), W, g):
+        w -= lr * dw
+        n = x.shape[0]
+        x8, sx = torch.empty(n, d_in, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+        w8, sw = torch.empty(d, d_in, dtype=torch.int8, device="cuda"), torch.empty(d, device="cuda")
+        rep = torch.empty(n, d, device="cuda")
+        binding.gc_quantize_rows(x, x8, sx)
+        binding.gc_quantize_rows(w, w8, sw)
+        binding.gc_matmul_i8(x8, sx, w8, sw, rep)
+        xd, wd = x.double(), w.double()
+        ex = (0.5 + 2.0 ** -16) * sx.double()[:, None]
+        ew = (0.5 + 2.0 ** -16) * sw.double()
+        limit = ex * wd.abs().sum(1) + ew * xd.abs().sum(1, keepdim=True) + d_in * ex * ew
+        assert bool(((rep.double() - xd @ wd.t()).abs() <= limit * (1 + 2.0 ** -20) + 2.0 ** -22 * rep.double().abs()).all())
+        reps.append(rep)
+    # scores of 8-bit representations, as distances of the tiled loss
+    q8 = [(torch.empty(r.shape, dtype=torch.int8, device="cuda"), torch.empty(r.shape[0], device="cuda")) for r in reps]
+    for r, (q, s) in zip(reps, q8):
+        binding.gc_quantize_rows(r, q, s)
+    cache = binding.DistanceCache(pos, B, N, tau)
+    scores = torch.empty(B, N, device="cuda")
+    binding.gc_matmul_i8(*q8[0], *q8[1], scores)
+    cache.accumulate(scores, 0, 0)
+    cache.finish()
+    torch.cuda.synchronize()
+    assert cache.dev_status.item() == 0
+    s64 = scores.double()
+    ref = (torch.logsumexp(s64, dim=1) - s64[torch.arange(B, device="cuda"), pos.long()]).mean().item()
+    assert abs(cache.loss.item() - ref) <= 1e-5 * abs(ref)
+    dense = reps[0].double() @ reps[1].double().t()
+    e = [(0.5 + 2.0 ** -16) * s.double() for _, s in q8]
+    limit = e[0][:, None] * reps[1].double().abs().sum(1) + e[1] * reps[0].double().abs().sum(1, keepdim=True) \
+        + d * e[0][:, None] * e[1]
+    assert bool(((s64 - dense).abs() <= limit * (1 + 2.0 ** -20) + 2.0 ** -22 * s64.abs()).all())

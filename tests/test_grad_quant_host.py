@@ -1,0 +1,171 @@
+"""Gradient norm, clipping, 8-bit rows and their product: what is refused before any device work, with
+addresses that are never read (no GPU needed)."""
+import ctypes
+
+import pytest
+import torch
+
+NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, LIMIT, ALIAS = 1, 2, 3, 5, 6, 9, 10
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2101_06983_b200 import _build
+    _build.build()
+    from paper_2101_06983_b200 import binding as b
+    return b
+
+
+def _list(binding, *tensors):
+    arr = (binding._Tensor * max(len(tensors), 1))()
+    for x, t in zip(arr, tensors):
+        a = dict(data=0x10000, out=None, rows=4, cols=64, ld=64, ld_out=64, dtype=0)
+        a.update(t)
+        for k, v in a.items():
+            setattr(x, k, v)
+    return arr, len(tensors)
+
+
+def _clip(binding, *tensors, max_norm=1.0, norm=0x100, ws=0x100000, wsb=1 << 20, n=None):
+    arr, count = _list(binding, *tensors)
+    return binding._lib.gc_grad_clip(arr, count if n is None else n, max_norm, None, norm, ws, wsb, None, None)
+
+
+def _norm(binding, *tensors, sq=0x200, norm=0x100, ws=0x100000, wsb=1 << 20):
+    arr, count = _list(binding, *tensors)
+    return binding._lib.gc_grad_norm(arr, count, sq, norm, ws, wsb, None, None)
+
+
+def _passes(status):
+    """Not refused for its arguments: without a B200 the call ends at the device."""
+    return status in (7, 8)
+
+
+needs_no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are not real ones")
+
+
+def test_lists_that_are_refused(binding):
+    assert _clip(binding, {}, norm=None) == NULL
+    assert _norm(binding, {}, sq=None, norm=None) == NULL
+    assert _clip(binding, dict(data=None)) == NULL
+    assert binding._lib.gc_grad_clip(None, 1, 1.0, None, 0x100, 0x100000, 1 << 20, None, None) == NULL
+    assert binding._lib.gc_grad_scale(_list(binding, {})[0], 1, None, 1.0, None, None) == NULL
+    assert _clip(binding, {}, n=-1) == SHAPE
+    assert _clip(binding, {}, max_norm=-1.0) == SHAPE
+    assert _clip(binding, {}, max_norm=float("nan")) == SHAPE
+    assert _clip(binding, dict(rows=-1)) == SHAPE
+    assert _clip(binding, dict(cols=-1)) == SHAPE
+    assert _clip(binding, dict(ld=63)) == SHAPE
+    assert _clip(binding, dict(ld=0)) == SHAPE                      # one row repeated
+    assert _clip(binding, dict(out=0x90000, ld_out=63)) == SHAPE
+    assert _clip(binding, dict(rows=1 << 40, cols=1 << 40, ld=1 << 40)) == SHAPE
+    assert _clip(binding, dict(rows=2, cols=(1 << 31) + 1, ld=(1 << 31) + 1)) == LIMIT
+    assert _clip(binding, {}, n=(1 << 20) + 1) == LIMIT
+    assert _clip(binding, dict(dtype=2)) == DTYPE
+    assert _clip(binding, dict(data=0x10002)) == ALIGN
+    assert _clip(binding, dict(data=0x10001, dtype=1)) == ALIGN
+    assert _clip(binding, dict(out=0x90002)) == ALIGN
+    assert _clip(binding, {}, ws=None) == WORKSPACE
+    assert _clip(binding, {}, ws=0x100010) == WORKSPACE
+    assert _clip(binding, {}, wsb=64) == WORKSPACE
+
+
+def test_places_that_two_tensors_share(binding):
+    assert _clip(binding, {}, {}) == ALIAS                          # the same tensor twice
+    assert _clip(binding, {}, dict(data=0x10000 + 4 * 255)) == ALIAS
+    assert _clip(binding, dict(data=0x10000 + 4 * 255), {}) == ALIAS
+    assert _clip(binding, dict(out=0x90000), dict(data=0x20000, out=0x90000)) == ALIAS
+    assert _clip(binding, dict(out=0x90000), dict(data=0x90000, out=0xa0000)) == ALIAS      # read and written
+    assert _clip(binding, dict(out=0x10100)) == ALIAS                # onto itself, further on
+    assert _clip(binding, dict(out=0x10000, rows=4, cols=32, ld=64, ld_out=32)) == ALIAS
+    a = dict(cols=32, ld=64)
+    assert _clip(binding, a, dict(a, data=0x10000 + 4 * 31)) == ALIAS
+    assert _clip(binding, a, dict(a, data=0x10000 + 4 * 33)) == ALIAS        # its rows end in the first's
+    assert _clip(binding, a, dict(a, data=0x10000 + 4 * 32, ld=60)) == ALIAS
+    # a long tensor with two inside it, the second not its neighbour in the order of addresses
+    assert _clip(binding, dict(rows=1, cols=1 << 12), dict(data=0x20000), dict(data=0x10000 + 4 * 2000)) == ALIAS
+
+
+@needs_no_gpu
+def test_lists_that_are_taken(binding):
+    assert _passes(_clip(binding))
+    assert _passes(_clip(binding, dict(data=None, rows=0)))
+    assert _passes(_clip(binding, {}, dict(data=0x10000 + 4 * 256)))
+    assert _passes(_clip(binding, dict(data=0x10000 + 4 * 256), {}))
+    assert _passes(_norm(binding, {}, {}))                           # read twice: counts twice
+    assert _passes(_clip(binding, dict(out=0x90000), dict(out=0xa0000)))
+    a = dict(cols=32, ld=64)
+    assert _passes(_clip(binding, a, dict(a, data=0x10000 + 4 * 32)))          # column halves of one matrix
+    assert _passes(_clip(binding, a, dict(data=0x10000 + 4 * 40, rows=1, cols=16, ld=0)))
+    assert _passes(_clip(binding, {}, max_norm=float("inf")))
+    assert _passes(_clip(binding, {}, max_norm=0.0))
+
+
+def test_workspace_of_a_list(binding):
+    assert binding.gc_grad_workspace_bytes(-1) == 0
+    assert binding.gc_grad_workspace_bytes((1 << 20) + 1) == 0
+    for n in (0, 1, 500, 1000, 1 << 20):
+        assert binding.gc_grad_workspace_bytes(n) > 0 and binding.gc_grad_workspace_bytes(n) % 256 == 0
+    assert binding.gc_grad_workspace_bytes(1 << 20) > binding.gc_grad_workspace_bytes(1)
+
+
+def test_lists_of_host_tensors_are_refused(binding):
+    with pytest.raises(ValueError):
+        binding.GradList([torch.zeros(4)])
+    with pytest.raises(ValueError):
+        binding.GradList([], out=[torch.zeros(4)])
+    with pytest.raises(ValueError):
+        binding.gc_quantize_rows(torch.zeros(2, 16), torch.zeros(2, 16, dtype=torch.int8), torch.zeros(2))
+
+
+def test_matrices_of_gradients(binding):
+    """How tensors are described: one row where they are dense, whatever the order of their dimensions."""
+    z = torch.zeros(6, 8, 4)
+    f = binding._as_matrix
+    assert f(z) == (1, 192, 192) and f(z.permute(2, 0, 1)) == (1, 192, 192)
+    assert f(z[0].t()) == (1, 32, 32)
+    assert f(z[0][:, :3]) == (8, 3, 4)
+    assert f(z[0][:, 1]) == (8, 1, 4)
+    assert f(z[0][:, 1:2]) == (8, 1, 4)
+    assert f(torch.zeros(())) == (1, 1, 1) and f(torch.zeros(0, 5)) == (1, 0, 0)
+    assert f(z[0], torch.zeros(8, 6)[:, :4]) == (8, 4, 4)
+    assert f(torch.zeros(1).expand(5)) == (5, 1, 0)                  # refused by the library
+    for bad in (z[:, :, :3], z[0][:, ::2]):
+        with pytest.raises(ValueError):
+            f(bad)
+    with pytest.raises(ValueError):
+        f(z[0].t(), torch.zeros(4, 8))
+
+
+def _quantize(binding, **over):
+    a = dict(X=0x10000, ldx=64, rows=4, d=64, dtype=0, q=0x20000, ldq=64, scale=0x30000)
+    a.update(over)
+    return binding._lib.gc_quantize_rows(*a.values(), None)
+
+
+def _matmul(binding, **over):
+    a = dict(A=0x10000, lda=64, sa=0x100, B=0x20000, ldb=64, sb=0x200, rows=4, cols=8, k=64, dtype=0, out=0x30000, ldo=8,
+             status=None)
+    a.update(over)
+    return binding._lib.gc_matmul_i8(*a.values(), None)
+
+
+def test_8_bit_calls_that_are_refused(binding):
+    assert _quantize(binding, X=None) == NULL and _quantize(binding, q=None) == NULL
+    assert _quantize(binding, scale=None) == NULL
+    assert _quantize(binding, dtype=2) == DTYPE
+    for bad in (dict(rows=0), dict(d=0), dict(ldx=63), dict(ldq=63)):
+        assert _quantize(binding, **bad) == SHAPE
+    for bad in (dict(X=0x10004), dict(ldx=66), dict(q=0x20008), dict(ldq=72), dict(dtype=1, ldx=68)):
+        assert _quantize(binding, **bad) == ALIGN
+    assert _quantize(binding, rows=(1 << 30) + 1) == LIMIT
+    for name in ("A", "B", "sa", "sb", "out"):
+        assert _matmul(binding, **{name: None}) == NULL
+    assert _matmul(binding, dtype=7) == DTYPE
+    for bad in (dict(rows=0), dict(cols=0), dict(k=0), dict(lda=63), dict(ldb=63), dict(ldo=7)):
+        assert _matmul(binding, **bad) == SHAPE
+    for bad in (dict(A=0x10008), dict(B=0x20008), dict(out=0x30008), dict(lda=72), dict(ldb=72), dict(ldo=9),
+                dict(dtype=1, ldo=12)):
+        assert _matmul(binding, **bad) == ALIGN
+    assert _matmul(binding, k=131072, lda=131072, ldb=131072) == LIMIT
+    assert _matmul(binding, cols=(1 << 30) + 1, ldo=(1 << 30) + 4) == LIMIT
