@@ -367,8 +367,9 @@ int gc_grad_clip(const gc_tensor* tensors, int64_t n_tensors, float max_norm, do
  * A trained encoder in 8-bit integers: the linear encoder f(s) = W s of Step 3 run forward, and the
  * products S = <Q_i, P_j> of stored rows (beside gc_dist_dot_block, whose blocks gc_dist_accumulate takes).
  *
- *   gc_quantize_rows   scale[i] = max_j |X[i][j]| / 127 (fp32) and q[i][j] = X[i][j] / scale[i] to the
- *                      nearest integer, ties to even (decided on the exact quotient).  A row of zeros, or
+ *   gc_quantize_rows   scale[i] = max_j |X[i][j]| times 1/127, in fp32 (the reciprocal rounded, then the
+ *                      product), and q[i][j] = X[i][j] / scale[i] to the nearest integer, ties to even (decided
+ *                      on the exact quotient), at most 127 in size.  A row of zeros, or
  *                      one whose scale rounds to zero, gets scale 0 and zeros; a row with a NaN or an
  *                      infinity gets scale NaN and zeros, so that its products are NaN.
  *   gc_matmul_i8       out[i][j] = (sum_k A[i][k] B[j][k]) a_scale[i] b_scale[j]: a scale for each row of A

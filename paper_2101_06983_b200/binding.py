@@ -575,7 +575,7 @@ def gc_grad_clip(grads, max_norm, norm, sq_sum=None, ws=None, dev_status=None) -
 
 
 def gc_quantize_rows(X, q, scale) -> None:
-    """scale[i] (float32) = max |X[i]| / 127 and q[i] (int8) = X[i] / scale[i] to the nearest integer."""
+    """scale[i] (float32) = max |X[i]| times 1/127 and q[i] (int8) = X[i] / scale[i] to the nearest integer."""
     if X.dim() != 2 or q.shape != X.shape or X.stride(1) != 1 or q.stride(1) != 1:
         raise ValueError("X and q must be 2-D of one shape with unit stride along their rows")
     rows, d = X.shape

@@ -22,6 +22,8 @@ namespace {
 constexpr int GR_THREADS = 512;
 constexpr int GR_TILE_UNITS = 1024;            // 16-byte vectors of a tile; single elements where they do not fit
 constexpr int GR_PER = GR_TILE_UNITS / GR_THREADS;
+constexpr int GR_DEEP = 4;                     // vectors of a thread under way
+constexpr int GR_BLOCKS = 3;                   // to an SM
 constexpr int GR_SLOTS = 1024;                 // partial sums of a launch
 constexpr double GR_EPS = 1e-6;
 
@@ -121,19 +123,33 @@ __device__ __forceinline__ int entry_of(const List<N>& list, uint32_t t) {
     }
     return lo;
 }
-// Where unit u of an entry lies, in elements from src (OUT: from dst).
-template <bool OUT>
-__device__ __forceinline__ int64_t place_of(const Entry& e, int64_t u) {
-    const int vec = e.bf16 ? 8 : 4;
-    if (e.mode == FLAT_VEC) return e.head + u * vec;
-    const int64_t r = u / e.cols, c = u - r * e.cols;
-    return r * (OUT ? e.ld_out : e.ld) + (e.mode == ROWS_VEC ? c * vec : c);
+// A tile of an entry that is no stretch of vectors: its first unit and where that lies.
+struct Tile {
+    int64_t r;
+    uint32_t c, n;        // row and column of the first unit; units of the tile
+};
+__device__ __forceinline__ Tile tile_of(const Entry& e, uint32_t t) {
+    const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS;
+    Tile x;
+    x.n = (uint32_t)min((int64_t)GR_TILE_UNITS, e.units - u);
+    x.r = u / e.cols;
+    x.c = (uint32_t)(u - x.r * e.cols);
+    return x;
+}
+// Where unit k of it lies, in elements from a base of pitch ld.
+__device__ __forceinline__ int64_t place_of(const Entry& e, const Tile& x, uint32_t k, int64_t ld) {
+    const uint32_t at = x.c + k, down = at / e.cols;      // (both below 2^31 + 2^10)
+    return (x.r + down) * ld + (int64_t)(at - down * e.cols) * (e.mode == ROWS_VEC ? (e.bf16 ? 8 : 4) : 1);
 }
 
 // The block's run of tiles.
 __device__ __forceinline__ void run_of(uint32_t tiles, uint32_t* lo, uint32_t* hi) {
     *lo = (uint32_t)((uint64_t)tiles * blockIdx.x / gridDim.x);
     *hi = (uint32_t)((uint64_t)tiles * (blockIdx.x + 1) / gridDim.x);
+}
+template <int N>
+__device__ __forceinline__ uint32_t end_of(const List<N>& list, int at) {
+    return at + 1 < list.n ? list.e[at + 1].first : list.tiles;
 }
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -152,7 +168,7 @@ __device__ __forceinline__ double block_sum(double v, double* part) {
 
 // part[block] = the sum of squares of the block's run of tiles.
 template <int N>
-__global__ void __launch_bounds__(GR_THREADS)
+__global__ void __launch_bounds__(GR_THREADS, GR_BLOCKS)
 grad_square_kernel(const __grid_constant__ List<N> list, double* part) {
     __shared__ double warp_part[GR_THREADS / 32];
     dep_release();
@@ -160,37 +176,58 @@ grad_square_kernel(const __grid_constant__ List<N> list, double* part) {
     uint32_t t, end;
     run_of(list.tiles, &t, &end);
     double sum = 0.0;
-    int at = t < end ? entry_of(list, t) : 0;
-    for (; t < end; ++t) {
-        while (at + 1 < list.n && list.e[at + 1].first <= t) ++at;
+    for (int at = t < end ? entry_of(list, t) : 0; t < end; ++at) {
         const Entry& e = list.e[at];
-        const int64_t u0 = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
-        if (e.mode == ELEM) {
-#pragma unroll
-            for (int i = 0; i < GR_PER; ++i) {
-                const int64_t u = u0 + i * GR_THREADS;
-                if (u < e.units) {
-                    const double x = load_one(e.src, place_of<false>(e, u), e.bf16);
-                    sum = fma(x, x, sum);
-                }
+        const uint32_t stop = min(end, end_of(list, at));
+        const bool bf16 = e.bf16;
+        if (e.mode == FLAT_VEC) {
+            const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4);
+            if (t == e.first && threadIdx.x < e.head + e.tail) {
+                const int k = threadIdx.x;
+                const double x = load_one(e.src, k < e.head ? k : k + e.units * (bf16 ? 8 : 4), bf16);
+                sum = fma(x, x, sum);
             }
+            const int64_t hi = min(e.units, (int64_t)(stop - e.first) * GR_TILE_UNITS);
+            int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
+            for (; u < hi; u += GR_DEEP * GR_THREADS) {
+                uint4 v[GR_DEEP];
+                if (u + (GR_DEEP - 1) * GR_THREADS < hi) {
+#pragma unroll
+                    for (int i = 0; i < GR_DEEP; ++i)
+                        v[i] = *reinterpret_cast<const uint4*>(src + 16 * (u + i * GR_THREADS));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < GR_DEEP; ++i)
+                        v[i] = u + i * GR_THREADS < hi ? *reinterpret_cast<const uint4*>(src + 16 * (u + i * GR_THREADS))
+                                                       : make_uint4(0, 0, 0, 0);
+                }
+                sum += square_sum(v, bf16);
+            }
+            t = stop;
             continue;
         }
-        uint4 v[GR_PER];
-        const int es = e.bf16 ? 2 : 4;
+        for (; t < stop; ++t) {
+            const Tile x = tile_of(e, t);
+            if (e.mode == ROWS_VEC) {
+                uint4 v[GR_PER];
 #pragma unroll
-        for (int i = 0; i < GR_PER; ++i) {
-            const int64_t u = u0 + i * GR_THREADS;
-            v[i] = u < e.units ? *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
-                                                                 place_of<false>(e, u) * es)
-                               : make_uint4(0, 0, 0, 0);
-        }
-        sum += square_sum(v, e.bf16);
-        if (t == e.first && threadIdx.x < e.head + e.tail) {
-            const int k = threadIdx.x;
-            const int64_t i = k < e.head ? k : k + e.units * (16 / es);
-            const double x = load_one(e.src, i, e.bf16);
-            sum = fma(x, x, sum);
+                for (int i = 0; i < GR_PER; ++i) {
+                    const uint32_t k = threadIdx.x + i * GR_THREADS;
+                    v[i] = k < x.n ? *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
+                                                                     place_of(e, x, k, e.ld) * (bf16 ? 2 : 4))
+                                   : make_uint4(0, 0, 0, 0);
+                }
+                sum += square_sum(v, bf16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < GR_PER; ++i) {
+                    const uint32_t k = threadIdx.x + i * GR_THREADS;
+                    if (k < x.n) {
+                        const double y = load_one(e.src, place_of(e, x, k, e.ld), bf16);
+                        sum = fma(y, y, sum);
+                    }
+                }
+            }
         }
     }
     sum = block_sum(sum, warp_part);
@@ -220,7 +257,7 @@ grad_norm_kernel(const double* part, int slots, double* sq_sum, float* norm, int
 
 // out = c g, c from the sum of `slots` partial sums.
 template <int N>
-__global__ void __launch_bounds__(GR_THREADS)
+__global__ void __launch_bounds__(GR_THREADS, GR_BLOCKS)
 grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int slots, float max_norm,
                   double* sq_sum, float* norm, int* dev_status, int tell) {
     __shared__ double warp_part[GR_THREADS / 32];
@@ -233,39 +270,66 @@ grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int 
     const double wide = (double)max_norm / (sqrt(total) + GR_EPS);
     const bool copy = !isfinite(total) || wide >= 1.0;
     const float c = (float)wide;
-    uint32_t t, end;
-    run_of(list.tiles, &t, &end);
-    int at = t < end ? entry_of(list, t) : 0;
-    for (; t < end; ++t) {
-        while (at + 1 < list.n && list.e[at + 1].first <= t) ++at;
+    uint32_t begin, t;
+    run_of(list.tiles, &begin, &t);
+    // backwards: what the sum of squares read last is in the L2 still
+    for (int at = begin < t ? entry_of(list, t - 1) : 0; t > begin; --at) {
         const Entry& e = list.e[at];
-        if (copy && e.src == e.dst) continue;           // the values stay as they are
-        const int64_t u0 = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
-        if (e.mode == ELEM) {
-#pragma unroll
-            for (int i = 0; i < GR_PER; ++i) {
-                const int64_t u = u0 + i * GR_THREADS;
-                if (u < e.units) {
-                    scale_one(e, place_of<false>(e, u), place_of<true>(e, u), copy, c);
-                }
-            }
+        const uint32_t start = max(begin, e.first);
+        const bool bf16 = e.bf16;
+        if (copy && e.src == e.dst) {                    // the values stay as they are
+            t = start;
             continue;
         }
-        const int es = e.bf16 ? 2 : 4;
+        if (e.mode == FLAT_VEC) {
+            const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4);
+            char* dst = static_cast<char*>(e.dst) + e.head * (bf16 ? 2 : 4);
+            const int64_t lo = (int64_t)(start - e.first) * GR_TILE_UNITS;
+            const int64_t hi = min(e.units, (int64_t)(t - e.first) * GR_TILE_UNITS);
+            constexpr int64_t STEP = GR_DEEP * GR_THREADS;
+            for (int64_t u = lo + (hi - lo - 1) / STEP * STEP + threadIdx.x; u >= lo && hi > lo; u -= STEP) {
+                uint4 v[GR_DEEP];
+                if (u + (GR_DEEP - 1) * GR_THREADS < hi) {
 #pragma unroll
-        for (int i = 0; i < GR_PER; ++i) {
-            const int64_t u = u0 + i * GR_THREADS;
-            if (u < e.units) {
-                const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
-                                                                place_of<false>(e, u) * es);
-                *reinterpret_cast<uint4*>(static_cast<char*>(e.dst) + place_of<true>(e, u) * es) =
-                    copy ? v : scale_vec(v, e.bf16, c);
+                    for (int i = 0; i < GR_DEEP; ++i)
+                        v[i] = *reinterpret_cast<const uint4*>(src + 16 * (u + i * GR_THREADS));
+#pragma unroll
+                    for (int i = 0; i < GR_DEEP; ++i)
+                        *reinterpret_cast<uint4*>(dst + 16 * (u + i * GR_THREADS)) =
+                            copy ? v[i] : scale_vec(v[i], bf16, c);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < GR_DEEP; ++i)
+                        if (u + i * GR_THREADS < hi) {
+                            v[i] = *reinterpret_cast<const uint4*>(src + 16 * (u + i * GR_THREADS));
+                            *reinterpret_cast<uint4*>(dst + 16 * (u + i * GR_THREADS)) =
+                                copy ? v[i] : scale_vec(v[i], bf16, c);
+                        }
+                }
             }
+            if (start == e.first && threadIdx.x < e.head + e.tail) {
+                const int k = threadIdx.x;
+                const int64_t i = k < e.head ? k : k + e.units * (bf16 ? 8 : 4);
+                scale_one(e, i, i, copy, c);
+            }
+            t = start;
+            continue;
         }
-        if (t == e.first && threadIdx.x < e.head + e.tail) {
-            const int k = threadIdx.x;
-            const int64_t i = k < e.head ? k : k + e.units * (16 / es);
-            scale_one(e, i, i, copy, c);
+        for (; t > start; --t) {
+            const Tile x = tile_of(e, t - 1);
+#pragma unroll
+            for (int i = 0; i < GR_PER; ++i) {
+                const uint32_t k = threadIdx.x + i * GR_THREADS;
+                if (k >= x.n) break;
+                const int64_t from = place_of(e, x, k, e.ld), to = place_of(e, x, k, e.ld_out);
+                if (e.mode == ROWS_VEC) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) + from * (bf16 ? 2 : 4));
+                    *reinterpret_cast<uint4*>(static_cast<char*>(e.dst) + to * (bf16 ? 2 : 4)) =
+                        copy ? v : scale_vec(v, bf16, c);
+                } else {
+                    scale_one(e, from, to, copy, c);
+                }
+            }
         }
     }
 }
@@ -435,7 +499,7 @@ int each_group(const gc_tensor* list, int64_t n, bool write, Go go) {
 }
 
 unsigned grid_for(uint32_t tiles) {
-    const uint32_t most = (uint32_t)std::min(GR_SLOTS, 4 * sm_count());
+    const uint32_t most = (uint32_t)std::min(GR_SLOTS, GR_BLOCKS * sm_count());
     return std::max(1u, std::min(tiles, most));
 }
 

@@ -1,6 +1,6 @@
 """gc_quantize_rows and gc_matmul_i8 against their definitions.
 
-Both are compared bit for bit.  The scale is one IEEE division of fp32 numbers, an 8-bit integer the nearest one to
+Both are compared bit for bit.  The scale is one fp32 product (with 1/127, rounded), an 8-bit integer the nearest one to
 the quotient of x and that scale, which fp64 holds closely enough to tell every side of every border.  A
 product is an integer below 2^31, rounded to fp32, and two fp32 products in a stated order, then one rounding
 to bf16 where that is the output's type."""
@@ -34,7 +34,7 @@ def _quantized(x):
     """The definition, on the host in 64 bits."""
     x = x.detach().cpu().float().numpy()
     amax = np.abs(x).max(axis=1)
-    scale = (amax / np.float32(127)).astype(np.float32)
+    scale = (amax * np.float32(1 / 127)).astype(np.float32)
     q = np.zeros(x.shape, np.int8)
     for i, s in enumerate(scale):
         if not np.isfinite(amax[i]):
@@ -80,7 +80,7 @@ def test_values_next_to_borders(binding, d, dtype):
     x = np.zeros((rows, d), np.float32)
     for i in range(rows):
         top = np.float32(2.0 ** gen.uniform(-30, 30))
-        s = np.float32(top / np.float32(127))
+        s = np.float32(top * np.float32(1 / 127))
         half = (gen.integers(-127, 127, d).astype(np.float64) + 0.5) * np.float64(s)
         v = half.astype(np.float32)
         v = (v.view(np.int32) + gen.integers(-2, 3, d).astype(np.int32)).view(np.float32)
@@ -284,7 +284,7 @@ def test_a_step_then_the_encoder_in_8_bits(binding):
     bits: representations, scores of queries against passages, and the loss of those scores.
 
     The tolerance of a representation: of k terms x w, each of x and w is off by at most half a step of its row, s / 2
-    (and 2^-24 of itself, from the scale's rounding); three fp32 roundings after that."""
+    (and what 127 s and the row's largest value differ by, 2^-23 of it); three fp32 roundings after that."""
     from paper_2101_06983_b200 import inputs
     B, N, d, d_in, tau = 256, 512, 128, 192, 1.0
     lr, bound = 0.5, 0.05
