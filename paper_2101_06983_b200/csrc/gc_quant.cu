@@ -4,14 +4,15 @@
 //     out_ij  = a_scale_i b_scale_j sum_k A_ik B_jk
 //
 // gc_quantize_rows is bound by memory: a row is read once (kept in registers), written at a byte per value.
-// gc_matmul_i8 runs on the tensor cores (tcgen05, kind::i8: exact products and 32-bit integer sums).  Rows of B
-// (channels, passages) are the M = 128 side of the products and rows of A (tokens, queries) the N side: a row of
-// B is then a lane of tensor memory, 32 lanes store 32 neighbouring outputs, and few rows of A
-// cost no more than their share of the instruction.
+// gc_matmul_i8 runs on the tensor cores (tcgen05, kind::i8: exact products and 32-bit integer sums).
 #include <cuda_bf16.h>
 #include <math.h>
 
 #include <algorithm>
+#ifdef IM_TUNE
+#include <stdio.h>
+#include <stdlib.h>
+#endif
 
 #include "tc_common.cuh"
 
@@ -22,6 +23,7 @@ namespace {
 // Rows to 8 bits
 // ---------------------------------------------------------------------------------------------------
 constexpr int QZ_THREADS = 256;
+constexpr int QZ_BLOCKS = 4;                // to an SM: 3 and 5 are 5 to 20 % slower for nearly all widths
 constexpr float MAGIC = 12582912.f;        // 1.5 * 2^23: adding it rounds to an integer, left in the low bits
 
 constexpr float RECIP_127 = 1.f / 127.f;   // rounded to fp32
@@ -62,89 +64,115 @@ if (BF16) {
     __device__ __forceinline__ uint32_t most(uint32_t m) const {
 #pragma unroll
         for (int e = 0; e < (BF16 ? 4 : 8); ++e)
-            m = BF16 ? __vmaxu2(m, w[e] & 0x7fff7fffu) : max(m, w[e] & 0x7fffffffu);
+            if (BF16) asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(w[e] & 0x7fff7fffu));
+            else      m = max(m, w[e] & 0x7fffffffu);
         return m;
     }
 };
-// The 8-bit integers of a piece.  x * inv misses x / scale by less than 2^-16 (both are at most 127.5, inv is off
-// by 2^-24 of itself): where one of the eight is nearer to a border than that, their quotients are formed in
-// fp64, where no two quotients of 24-bit numbers on different sides of a border are the same.
+// The 8-bit integers of a piece.  r, x * inv rounded to an integer, is the nearest one to x / scale if the remainder
+// x - r scale is below half a scale.  The remainder is exact (one fused multiply-add: x * inv misses the
+// quotient by less than 2^-15, and the difference has no bits below half of scale's last), so where one of the eight
+// is that large, comparing it with scale / 2 decides.  Rows of scales below 2^-100, whose 1 / s may be infinite, form
+// the quotients in fp64.
+__device__ __noinline__ uint32_t exact_i8(float x, float scale) {
+    const double q = rint((double)x / (double)scale);
+    return (uint32_t)(int)fmin(fmax(q, -127.0), 127.0);
+}
 template <bool BF16>
 __device__ __forceinline__ uint2 to_i8(const Piece<BF16>& x, float inv, float scale, bool wide) {
     uint32_t m[8];
-    float off = 0.f;
+    float most = 0.f;
+    const uint64_t inv2 = pack2(inv, inv), magic2 = pack2(MAGIC, MAGIC), minus2 = pack2(-1.f, -1.f);
+    const uint64_t scale2 = pack2(scale, scale);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float v = x.at(e), t = fmaf(v, inv, MAGIC);
-        m[e] = __float_as_uint(t);
-        off = fmaxf(off, fabsf(fmaf(v, inv, -(t - MAGIC))));
+    for (int e = 0; e < 8; e += 2) {
+        const uint64_t v = pack2(x.at(e), x.at(e + 1)), t = fma2(v, inv2, magic2);
+        float a, b;
+        unpack2(fma2(fma2(t, minus2, magic2), scale2, v), a, b);
+        most = fmaxf(most, fmaxf(fabsf(a), fabsf(b)));
+        unpack2(t, a, b);
+        m[e] = __float_as_uint(a);
+        m[e + 1] = __float_as_uint(b);
     }
-    if (wide || off > 0.49998f) {
-#pragma unroll 1
+    if (wide) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m[e] = exact_i8(x.at(e), scale);
+    } else if (most >= 0.5f * scale) {
+        const float half = 0.5f * scale;
+#pragma unroll
         for (int e = 0; e < 8; ++e) {
-            uint32_t word = x.w[0];                    // (a fixed index: the piece stays in registers)
-#pragma unroll
-            for (int k = 1; k < (BF16 ? 4 : 8); ++k) if (k == (BF16 ? e >> 1 : e)) word = x.w[k];
-            const float v = __uint_as_float(!BF16 ? word : e & 1 ? word & 0xffff0000u : word << 16);
-            const double q = rint((double)v / (double)scale);
-            const uint32_t r = (uint32_t)(int)fmin(fmax(q, -127.0), 127.0);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) if (k == e) m[k] = r;
+            const float rest = fmaf(MAGIC - __uint_as_float(m[e]), scale, x.at(e)), far = fabsf(rest);
+            if (far > half || (far == half && (m[e] & 1u))) m[e] += rest > 0.f ? 1u : 0xffffffffu;
         }
     }
     return make_uint2(__byte_perm(__byte_perm(m[0], m[1], 0x0040), __byte_perm(m[2], m[3], 0x0040), 0x5410),
                       __byte_perm(__byte_perm(m[4], m[5], 0x0040), __byte_perm(m[6], m[7], 0x0040), 0x5410));
 }
 
-// WARPS warps to a row; a lane holds KEEP pieces of 8 values of it in registers, the next row's under way
-// meanwhile, and reads what is beyond them twice.
-template <bool BF16, int WARPS, int KEEP>
-__global__ void __launch_bounds__(QZ_THREADS)
+// 1 / s within 2^-22 of itself.  bf16 rows: on the side of it that s = amax / 127 (1 - eps) is off to.  Such rows are full
+// of values with 127 x / amax = h halfway between two integers: x / s is then h (1 + eps), and x * inv = h (1 + eps) s inv lies
+// on the same side of h if s inv - 1 is not of the other sign.  Without this nearly every piece of a warp has a
+// value whose first integer is wrong (131072 x 768: 61 us, with it 55).
+template <bool BF16>
+__device__ __forceinline__ float reciprocal(float s, float amax) {
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    if (!BF16) return inv;
+    const float eps = fmaf(-127.f, s, amax), off = fmaf(s, inv, -1.f);
+    const uint32_t step = eps > 0.f && off < 0.f ? 1u : eps < 0.f && off > 0.f ? 0xffffffffu : 0u;
+    return __uint_as_float(__float_as_uint(inv) + step);
+}
+
+// LANES lanes (8, 16, a warp or several) to a row; a lane holds KEEP pieces of 8 values of it in registers and reads
+// what is beyond them twice.
+template <bool BF16, int LANES, int KEEP>
+__global__ void __launch_bounds__(QZ_THREADS, QZ_BLOCKS)
 quantize_rows_kernel(const void* X, int64_t ldx, int64_t rows, int64_t d, int8_t* q, int64_t ldq, float* scale) {
-    constexpr int PER_BLOCK = QZ_THREADS / 32 / WARPS, STEP = 32 * WARPS * 8;
+    constexpr int PER_BLOCK = QZ_THREADS / LANES, STEP = LANES * 8, WARPS = LANES / 32;
     __shared__ uint32_t warp_max[2][QZ_THREADS / 32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t k0 = 8 * (lane + 32 * (warp % WARPS)), pitch = ldx * (BF16 ? 2 : 4);
-    const int64_t by = (int64_t)gridDim.x * PER_BLOCK;
+    const int lane = threadIdx.x % LANES, warp = threadIdx.x >> 5;
+    const int64_t k0 = 8 * lane, pitch = ldx * (BF16 ? 2 : 4);
     dep_release();
     dep_wait();
     int turn = 0;
-    int64_t i = blockIdx.x * (int64_t)PER_BLOCK + warp / WARPS;
-    Piece<BF16> x[KEEP], next[KEEP];
-    auto fetch = [&](int64_t row) {
-        const char* src = static_cast<const char*>(X) + row * pitch;
-#pragma unroll
-        for (int c = 0; c < KEEP; ++c) next[c].load(src, k0 + (int64_t)c * STEP, d);
-    };
-    if (i < rows) fetch(i);
-    for (; i < rows; i += by) {
-        const char* src = static_cast<const char*>(X) + i * pitch;
-#pragma unroll
-        for (int c = 0; c < KEEP; ++c) x[c] = next[c];
-        if (i + by < rows) fetch(i + by);
+    for (int64_t first = blockIdx.x * (int64_t)PER_BLOCK; first < rows; first += (int64_t)gridDim.x * PER_BLOCK) {
+        const int64_t i = first + threadIdx.x / LANES;
+        const bool live = i < rows;
+        const char* src = static_cast<const char*>(X) + (live ? i : first) * pitch;
+        Piece<BF16> x[KEEP];
         uint32_t most = 0;
 #pragma unroll
+        for (int c = 0; c < KEEP; ++c) x[c].load(src, k0 + c * STEP, d);
+#pragma unroll
         for (int c = 0; c < KEEP; ++c) most = x[c].most(most);
-        for (int64_t k = k0 + (int64_t)KEEP * STEP; k < d; k += STEP) {
-            Piece<BF16> v;
-            v.load(src, k, d);
-            most = v.most(most);
+        if (LANES == QZ_THREADS) {
+            for (int64_t k = k0 + KEEP * STEP; k < d; k += STEP) {
+                Piece<BF16> v;
+                v.load(src, k, d);
+                most = v.most(most);
+            }
         }
         if (BF16) most = max(most & 0xffff0000u, most << 16);
-        most = __reduce_max_sync(0xffffffffu, most);
-        if (WARPS > 1) {                   // (all rows of a block end together: one row to a block)
-            if (lane == 0) warp_max[turn][warp] = most;
+        if (LANES < 32) {
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+        } else {
+            most = __reduce_max_sync(0xffffffffu, most);
+        }
+        if (WARPS > 1) {                   // (the blocks' rows end together: all threads come here equally often)
+            if ((threadIdx.x & 31) == 0) warp_max[turn][warp] = most;
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) most = max(most, warp_max[turn][w]);
+            for (int w = 0; w < WARPS; ++w) most = max(most, warp_max[turn][warp / WARPS * WARPS + w]);
             turn ^= 1;
         }
         const bool bad = most >= 0x7f800000u;
         const float s = bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(most) * RECIP_127;
         const bool none = bad || s == 0.f;
         const bool wide = s < 0x1p-100f;   // 1 / s may be infinite, s itself of few bits
-        const float inv = none || wide ? 0.f : 1.f / s;
-        if (lane == 0 && warp % WARPS == 0) scale[i] = s;
+        const float inv = none || wide ? 0.f : reciprocal<BF16>(s, __uint_as_float(most));
+        if (!live) continue;
+        if (lane == 0) scale[i] = s;
         int8_t* dst = q + i * ldq;
         auto put = [&](int64_t k, const Piece<BF16>& v) {
             if (k >= d) return;
@@ -158,11 +186,13 @@ quantize_rows_kernel(const void* X, int64_t ldx, int64_t rows, int64_t d, int8_t
             }
         };
 #pragma unroll
-        for (int c = 0; c < KEEP; ++c) put(k0 + (int64_t)c * STEP, x[c]);
-        for (int64_t k = k0 + (int64_t)KEEP * STEP; k < d; k += STEP) {
-            Piece<BF16> v;
-            v.load(src, k, d);
-            put(k, v);
+        for (int c = 0; c < KEEP; ++c) put(k0 + c * STEP, x[c]);
+        if (LANES == QZ_THREADS) {
+            for (int64_t k = k0 + KEEP * STEP; k < d; k += STEP) {
+                Piece<BF16> v;
+                v.load(src, k, d);
+                put(k, v);
+            }
         }
     }
 }
@@ -174,16 +204,24 @@ constexpr int IM_KB = 128;                 // contraction depth of a ring stage:
 constexpr int IM_MAX_ST = 11;
 constexpr size_t IM_SMEM = 225 * 1024;
 
+// The product as the tensor cores see it: rows of the M side (128 to a CTA) are lanes of tensor memory, rows of the
+// N side (bn to a tile) its columns.
+//   staged     M: A (tokens), N: B (channels).  A lane holds neighbouring outputs of a row; blocks of 32 rows x 128 bytes
+//              leave through shared memory with bulk tensor stores.
+//   otherwise  M: B, N: A.  32 lanes hold neighbouring outputs and store them as they are: for few rows of A, which
+//              cost no more than their share of the instruction.
 struct ImParams {
-    int64_t rows, cols;                    // of A (tokens), of B (channels)
+    int64_t rows_m, rows_n;
     int kblocks;
-    int bn;                                // rows of A in a tile: a multiple of 16 (pairs: of 32) up to 256
+    int bn;                                // rows of the N side in a tile: a multiple of 16 (pairs: of 32; staged: of
+                                           // 128 bytes of output) up to 256
     int stages;
-    int tiles_a, tiles_b;
-    const float* a_scale;
-    const float* b_scale;
+    int tiles_m, tiles_n;
+    const float* m_scale;
+    const float* n_scale;
     void* out;
     int64_t ldo;
+    int64_t whole;                         // staged: columns in whole 16 bytes, which is what bulk stores write
     int* dev_status;
 };
 struct ImBars {
@@ -221,8 +259,8 @@ __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint32_t a_lo, uint32_t 
     }
 }
 
-// One block of G rows of A x this warp's 32 rows of B: v the sums (column e: row of A), sa the scale of row `lane`
-// of the block.  Stores `n` of the G rows, the first at `row`.
+// Not staged: one block of G rows of A x this warp's 32 rows of B: v the sums (column e: row of A), sa the scale of
+// row `lane` of the block.  Stores `n` of the G rows, the first at `row`.
 template <int G, bool BF16>
 __device__ __forceinline__ void store_block(const uint32_t (&v)[G], float sa, float sb, const ImParams& p, int64_t row,
                                             int n, int64_t j, int lane) {
@@ -234,20 +272,20 @@ __device__ __forceinline__ void store_block(const uint32_t (&v)[G], float sa, fl
         const int odd = lane & 1;
         const int64_t jj = j - odd;
         __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.out) + (row + odd) * p.ldo + jj;
-        const bool both = jj + 1 < p.cols;
+        const bool both = jj + 1 < p.rows_m;
 #pragma unroll
         for (int e = 0; e < G; e += 2) {
             const float got = __shfl_xor_sync(0xffffffffu, odd ? f[e] : f[e + 1], 1);
             const __nv_bfloat162 w = odd ? __floats2bfloat162_rn(got, f[e + 1]) : __floats2bfloat162_rn(f[e], got);
             if (e + odd < n) {
                 if (both) *reinterpret_cast<__nv_bfloat162*>(dst) = w;
-                else if (jj < p.cols) *dst = w.x;
+                else if (jj < p.rows_m) *dst = w.x;
             }
             dst += 2 * p.ldo;
         }
     } else {
         float* dst = static_cast<float*>(p.out) + row * p.ldo + j;
-        if (j < p.cols) {
+        if (j < p.rows_m) {
 #pragma unroll
             for (int e = 0; e < G; ++e) {
                 if (e < n) *dst = f[e];
@@ -257,12 +295,12 @@ __device__ __forceinline__ void store_block(const uint32_t (&v)[G], float sa, fl
     }
 }
 
-// PAIR: a cluster of two CTAs owns 256 rows of B x bn rows of A, 128 of B and half of A's loaded by each CTA, which
-// holds the accumulators of its 128; otherwise a CTA owns 128 x bn.
-template <bool PAIR, bool BF16>
+// PAIR: a cluster of two CTAs owns 256 rows of the M side x bn of the N side, 128 and half of bn loaded by each CTA,
+// which holds the accumulators of its 128; otherwise a CTA owns 128 x bn.
+template <bool PAIR, bool BF16, bool STAGED>
 __global__ void __launch_bounds__(NTHREADS, 1)
-matmul_i8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-                 const ImParams p) {
+matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant__ CUtensorMap mapN,
+                 const __grid_constant__ CUtensorMap mapO, const ImParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) ImBars bars;
     __shared__ uint32_t tmem_s;
@@ -272,8 +310,8 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     const int lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)cluster_ctarank() : 0;
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const int a_rows = PAIR ? p.bn / 2 : p.bn;                 // of A that this CTA loads
-    const uint32_t stage_bytes = CHUNK_BYTES + (uint32_t)a_rows * 128u;
+    const int n_rows = PAIR ? p.bn / 2 : p.bn;                 // of the N side that this CTA loads
+    const uint32_t stage_bytes = CHUNK_BYTES + (uint32_t)n_rows * 128u;
     if (threadIdx.x == 0) {
         abort_s = 0;
         for (int s = 0; s < IM_MAX_ST; ++s) {
@@ -306,38 +344,38 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     dep_release();
     dep_wait();
 
-    const int64_t total = (int64_t)p.tiles_a * p.tiles_b;
+    const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
     const int64_t first = PAIR ? blockIdx.x >> 1 : blockIdx.x, by = PAIR ? gridDim.x >> 1 : gridDim.x;
-    constexpr int B_ROWS = PAIR ? 256 : 128;
+    constexpr int M_ROWS = PAIR ? 256 : 128;
     // the side of fewer tiles runs fastest: its rows stay in the L2 while the other side's pass once
-    auto tile_at = [&](int64_t t, int* ta, int* tb) {
-        if (p.tiles_a <= p.tiles_b) { *tb = (int)(t / p.tiles_a); *ta = (int)(t - (int64_t)*tb * p.tiles_a); }
-        else                        { *ta = (int)(t / p.tiles_b); *tb = (int)(t - (int64_t)*ta * p.tiles_b); }
+    auto tile_at = [&](int64_t t, int* tm, int* tn) {
+        if (p.tiles_n <= p.tiles_m) { *tm = (int)(t / p.tiles_n); *tn = (int)(t - (int64_t)*tm * p.tiles_n); }
+        else                        { *tn = (int)(t / p.tiles_m); *tm = (int)(t - (int64_t)*tn * p.tiles_m); }
     };
 
     if (warp < NPROD) {
-        const bool is_b = warp == 0;       // warp 0: rows of B, warp 1: rows of A
-        const uint32_t bytes = is_b ? CHUNK_BYTES : (uint32_t)a_rows * 128u;
+        const bool is_m = warp == 0;       // warp 0: the M side, warp 1: the N side
+        const uint32_t bytes = is_m ? CHUNK_BYTES : (uint32_t)n_rows * 128u;
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (int64_t t = first; t < total && ok; t += by) {
-            int ta, tb;
-            tile_at(t, &ta, &tb);
-            const int row = is_b ? tb * B_ROWS + rank * 128 : ta * p.bn + rank * a_rows;
+            int tm, tn;
+            tile_at(t, &tm, &tn);
+            const int row = is_m ? tm * M_ROWS + rank * 128 : tn * p.bn + rank * n_rows;
             for (int kb = 0; kb < p.kblocks; ++kb) {
                 ok = mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag);
                 if (!ok) break;
                 const uint32_t full = smem_u32(&bars.full[stage]);
-                const uint32_t dst = smem + stage * stage_bytes + (is_b ? 0u : CHUNK_BYTES);
+                const uint32_t dst = smem + stage * stage_bytes + (is_m ? 0u : CHUNK_BYTES);
                 const uint32_t full_leader = PAIR ? mapa_u32(full, 0) : full;
                 if (elect_one()) {
                     if (PAIR) {
                         if (rank == 0) mbar_expect_tx(full, 2 * bytes);
-                        tma_load_2d_pair(dst, is_b ? &mapB : &mapA, kb * IM_KB, row, full_leader);
+                        tma_load_2d_pair(dst, is_m ? &mapM : &mapN, kb * IM_KB, row, full_leader);
                     } else {
                         mbar_expect_tx(full, bytes);
-                        tma_load_2d(dst, is_b ? &mapB : &mapA, kb * IM_KB, row, full);
+                        tma_load_2d(dst, is_m ? &mapM : &mapN, kb * IM_KB, row, full);
                     }
                 }
                 if (++stage == p.stages) { stage = 0; phase ^= 1u; }
@@ -366,11 +404,11 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     ok = mbar_wait(smem_u32(&bars.full[stage]), phase, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t b = desc_lo(smem + stage * stage_bytes, 0);
-                    const uint32_t a = desc_lo(smem + stage * stage_bytes + CHUNK_BYTES, 0);
+                    const uint32_t m = desc_lo(smem + stage * stage_bytes, 0);
+                    const uint32_t n = desc_lo(smem + stage * stage_bytes + CHUNK_BYTES, 0);
                     if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) mma_i8<PAIR>(acc, b + 2 * k, a + 2 * k, idesc, kb != 0 || k != 0);
+                        for (int k = 0; k < 4; ++k) mma_i8<PAIR>(acc, m + 2 * k, n + 2 * k, idesc, kb != 0 || k != 0);
                         if (PAIR) {
                             tc_commit_pair(smem_u32(&bars.empty[stage]));
                             if (kb == p.kblocks - 1) tc_commit_pair(smem_u32(&bars.acc_full[use & 1]));
@@ -391,29 +429,122 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 if (ok && elect_one()) mbar_arrive_cluster(mapa_u32(smem_u32(&bars.acc_free_peer[use & 1]), 0));
             }
         }
+    } else if (STAGED) {
+        // warp: 32 rows of A (a quarter of the lanes), every other block of WIDE columns (128 bytes of output)
+        constexpr int WIDE = BF16 ? 64 : 32, BLOCKS = 256 / WIDE / 2;
+        const int q = warp & 3, ew = warp - (NPROD + 1), half = ew >> 2;
+        const uint32_t slot = smem + p.stages * stage_bytes + (uint32_t)ew * (2 * 4096u);
+        const uint32_t scales = smem + p.stages * stage_bytes + NSOFT * 2 * 4096u + (uint32_t)ew * 512u;
+        int use = 0, sent = 0;
+        for (int64_t t = first; t < total; t += by, ++use) {
+            int tm, tn;
+            tile_at(t, &tm, &tn);
+            const int64_t row0 = (int64_t)tm * M_ROWS + rank * 128 + 32 * q, i = row0 + lane;
+            const int64_t j0 = (int64_t)tn * p.bn;
+            const int n = (int)min((int64_t)p.bn, p.rows_n - j0);
+            const float sa = i < p.rows_m ? p.m_scale[i] : 0.f;
+            // the scales of this warp's columns, block after block
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int c = 32 * x + lane, col = (2 * (c / WIDE) + half) * WIDE + c % WIDE;
+                const float sb = col < n ? p.n_scale[j0 + col] : 0.f;
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + 4 * c), "f"(sb) : "memory");
+            }
+            __syncwarp();
+            if (!mbar_wait(smem_u32(&bars.acc_full[use & 1]), (uint32_t)(use >> 1) & 1u, abort_flag)) break;
+            tc_fence_after();
+            const uint32_t src = tmem + (use & 1) * 256 + ((uint32_t)(32 * q) << 16);
+            if (row0 < p.rows_m) {
+#pragma unroll 1
+                for (int x = 0; x < BLOCKS; ++x) {
+                    const int c = (2 * x + half) * WIDE;
+                    if (c >= n) break;
+                    const uint32_t buf = slot + (uint32_t)(sent & 1) * 4096u;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    __syncwarp();
+#pragma unroll
+                    for (int h = 0; h < WIDE / 32; ++h) {
+                        uint32_t v[32];
+                        tmem_ld32(src + c + 32 * h, v);
+                        tmem_ld_wait();
+                        float f[32];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            float s0, s1, s2, s3;
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                         : "=f"(s0), "=f"(s1), "=f"(s2), "=f"(s3)
+                                         : "r"(scales + 4 * (x * WIDE + 32 * h + e)));
+                            f[e] = (float)(int)v[e] * sa * s0;
+                            f[e + 1] = (float)(int)v[e + 1] * sa * s1;
+                            f[e + 2] = (float)(int)v[e + 2] * sa * s2;
+                            f[e + 3] = (float)(int)v[e + 3] * sa * s3;
+                        }
+                        if (j0 + c + 32 * h + 32 > p.whole && p.whole < p.rows_n && i < p.rows_m) {
+                            // the columns after the last whole 16 bytes
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const int64_t j = j0 + c + 32 * h + e;
+                                if (j >= p.whole && j < p.rows_n) {
+                                    if (BF16) static_cast<__nv_bfloat16*>(p.out)[i * p.ldo + j] = __float2bfloat16_rn(f[e]);
+                                    else      static_cast<float*>(p.out)[i * p.ldo + j] = f[e];
+                                }
+                            }
+                        }
+                        // 16-byte chunk k of row r lies at chunk k ^ (r & 7): the map's 128-byte swizzle
+#pragma unroll
+                        for (int k = 0; k < (BF16 ? 4 : 8); ++k) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                if (BF16) {
+                                    const __nv_bfloat162 b = __floats2bfloat162_rn(f[8 * (k & 3) + 2 * y],
+                                                                                   f[8 * (k & 3) + 2 * y + 1]);
+                                    w[y] = *reinterpret_cast<const uint32_t*>(&b);
+                                } else {
+                                    w[y] = __float_as_uint(f[4 * k + y]);
+                                }
+                            }
+                            const uint32_t at = buf + lane * 128 + (((4 * (BF16 ? h : 0) + k) ^ (lane & 7)) << 4);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                         ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (j0 + c < p.whole) {
+                        if (lane == 0) tma_store_2d(&mapO, buf, (int)(j0 + c), (int)row0);
+                        ++sent;
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.acc_free[use & 1]));
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
     } else {
         // warp: 32 rows of B (a quarter of the lanes), every other block of 32 rows of A (16 in small tiles)
         const int q = warp & 3, half = (warp - (NPROD + 1)) >> 2;
         const int block = p.bn >= 64 ? 32 : 16;
         int use = 0;
         for (int64_t t = first; t < total; t += by, ++use) {
-            int ta, tb;
-            tile_at(t, &ta, &tb);
-            const int64_t j = (int64_t)tb * B_ROWS + rank * 128 + 32 * q + lane;       // this lane's row of B
-            const int64_t i0 = (int64_t)ta * p.bn;
-            const int n = (int)min((int64_t)p.bn, p.rows - i0);
-            const float sb = j < p.cols ? p.b_scale[j] : 0.f;
+            int tm, tn;
+            tile_at(t, &tm, &tn);
+            const int64_t row0 = (int64_t)tm * M_ROWS + rank * 128 + 32 * q, j = row0 + lane;   // this lane's row of B
+            const int64_t i0 = (int64_t)tn * p.bn;
+            const int n = (int)min((int64_t)p.bn, p.rows_n - i0);
+            const float sb = j < p.rows_m ? p.m_scale[j] : 0.f;
             float sa[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const int c = (2 * x + half) * block + lane;
-                sa[x] = c < n ? p.a_scale[i0 + c] : 0.f;
+                sa[x] = c < n ? p.n_scale[i0 + c] : 0.f;
             }
             if (!mbar_wait(smem_u32(&bars.acc_full[use & 1]), (uint32_t)(use >> 1) & 1u, abort_flag)) break;
             tc_fence_after();
             const uint32_t src = tmem + (use & 1) * 256 + ((uint32_t)(32 * q) << 16);
-            const int64_t wrow = (int64_t)tb * B_ROWS + rank * 128 + 32 * q;           // the warp's first
-            if (wrow < p.cols) {
+            if (row0 < p.rows_m) {
                 if (block == 32) {
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
@@ -498,30 +629,54 @@ int check_device(int* dev) {
     return *dev < 0 || *dev >= 64 ? GC_ERR_CUDA : GC_OK;
 }
 
-struct ImPlan { bool pair; int bn; };
+// Row-major output of whole 16 bytes, boxes of 32 rows x 128 bytes, 128-byte swizzle; what lies past the ends is
+// not written.
+bool make_map_out(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t ld, bool bf16) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * (bf16 ? 2 : 4)};
+    cuuint32_t box[2] = {bf16 ? 64u : 32u, 32};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides,
+              box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct ImPlan { bool pair, staged; int bn; };
 
 // The tile that costs least by a count of cycles: rounds of tiles, each its products, its loads (85 bytes a
-// cycle) or its stores (20), whichever is longest, and the stores of the last one.
+// cycle) or its stores, whichever is longest, and the stores of the last one.
 ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, int out_dtype) {
-    ImPlan best{false, 16};
+    ImPlan best{false, false, 16};
+#ifdef IM_TUNE
+    if (getenv("IM_PLAN")) {
+        int a, b, c;
+        sscanf(getenv("IM_PLAN"), "%d,%d,%d", &a, &b, &c);
+        return ImPlan{a != 0, b != 0, c};
+    }
+#endif
     double least = INFINITY;
     const double kblocks = (double)((k + IM_KB - 1) / IM_KB);
-    const int most = (int)std::min<int64_t>(256, (rows + 15) / 16 * 16);
-    for (int pair = 0; pair < 2; ++pair)
-        for (int bn = pair ? 32 : 16; bn <= 256; bn += pair ? 32 : 16) {
-            if (bn >= most + (pair ? 32 : 16)) break;
-            const int64_t ta = (rows + bn - 1) / bn, tb = (cols + (pair ? 255 : 127)) / (pair ? 256 : 128);
-            const int64_t units = sm_count() / (pair ? 2 : 1);
-            const double rounds = (double)((ta * tb + units - 1) / units);
-            const double products = pair ? std::max(2.0 * bn, 190.0) : 4 * (bn / 2.0 + 44);
-            const double loads = (CHUNK_BYTES + 128.0 * (pair ? bn / 2 : bn)) / 85;
-            const double stores = 128.0 * bn * (out_dtype == GC_BF16 ? 2 : 4) / 20;
-            const double cost = rounds * std::max(kblocks * std::max(products, loads), stores) + stores;
-            if (cost < least) {
-                least = cost;
-                best = {pair != 0, bn};
+    for (int staged = 0; staged < (cols >= 8 ? 2 : 1); ++staged) {
+        const int64_t m = staged ? rows : cols, n = staged ? cols : rows;
+        for (int pair = 0; pair < 2; ++pair)
+            // (a staged block of 128 bytes must not reach into the next tile)
+            for (int step = staged ? (out_dtype == GC_BF16 ? 64 : 32) : pair ? 32 : 16, bn = step;
+                 bn <= 256 && bn < n + step; bn += step) {
+                const int64_t tn = (n + bn - 1) / bn, tm = (m + (pair ? 255 : 127)) / (pair ? 256 : 128);
+                const int64_t units = sm_count() / (pair ? 2 : 1);
+                const double rounds = (double)((tm * tn + units - 1) / units);
+                const double products = pair ? std::max(2.0 * bn, 190.0) : 4 * (bn / 2.0 + 44);
+                const double loads = (CHUNK_BYTES + 128.0 * (pair ? bn / 2 : bn)) / 85;
+                const double stores = 128.0 * bn * (out_dtype == GC_BF16 ? 2 : 4) / (staged ? 25 : 10);
+                const double cost = rounds * std::max(kblocks * std::max(products, loads), stores) + stores;
+                if (cost < least) {
+                    least = cost;
+                    best = {pair != 0, staged != 0, bn};
+                }
             }
-        }
+    }
     return best;
 }
 
@@ -547,13 +702,19 @@ int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dt
                               ldq, scale);
     };
     cudaError_t e;
-#define GC_QUANTIZE(BF16)                                                                                   \
-    (d <= 256 ? go(quantize_rows_kernel<BF16, 1, 1>, 8) : d <= 512 ? go(quantize_rows_kernel<BF16, 1, 2>, 8) \
-     : d <= 768 ? go(quantize_rows_kernel<BF16, 1, 3>, 8) : d <= 1024 ? go(quantize_rows_kernel<BF16, 1, 4>, 8) \
-     : d <= 2048 ? go(quantize_rows_kernel<BF16, 8, 1>, 1) : d <= 4096 ? go(quantize_rows_kernel<BF16, 8, 2>, 1) \
-                 : go(quantize_rows_kernel<BF16, 8, 4>, 1))
-    e = dtype == GC_BF16 ? GC_QUANTIZE(true) : GC_QUANTIZE(false);
-#undef GC_QUANTIZE
+#define GC_QZ(LANES, KEEP)                                                      \
+    (dtype == GC_BF16 ? go(quantize_rows_kernel<true, LANES, KEEP>, QZ_THREADS / LANES) \
+                      : go(quantize_rows_kernel<false, LANES, KEEP>, QZ_THREADS / LANES))
+    if (d <= 64) e = GC_QZ(8, 1);
+    else if (d <= 128) e = GC_QZ(8, 2);
+    else if (d <= 256) e = GC_QZ(16, 2);
+    else if (d <= 512) e = GC_QZ(32, 2);
+    else if (d <= 768) e = GC_QZ(32, 3);
+    else if (d <= 1024) e = GC_QZ(32, 4);
+    else if (d <= 2048) e = GC_QZ(64, 4);
+    else if (d <= 4096) e = GC_QZ(128, 4);
+    else e = GC_QZ(256, 4);
+#undef GC_QZ
     if (e != cudaSuccess) {
         cudaGetLastError();
         return GC_ERR_CUDA;
@@ -574,20 +735,32 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     int dev;
     if ((rc = check_device(&dev))) return rc;
     const ImPlan pl = make_im_plan(rows, cols, k, out_dtype);
+    const bool bf16 = out_dtype == GC_BF16;
     ImParams p{};
-    p.rows = rows; p.cols = cols;
+    p.rows_m = pl.staged ? rows : cols;
+    p.rows_n = pl.staged ? cols : rows;
+    p.m_scale = pl.staged ? a_scale : b_scale;
+    p.n_scale = pl.staged ? b_scale : a_scale;
     p.kblocks = (int)((k + IM_KB - 1) / IM_KB);
     p.bn = pl.bn;
-    p.tiles_a = (int)((rows + p.bn - 1) / p.bn);
-    p.tiles_b = (int)((cols + (pl.pair ? 255 : 127)) / (pl.pair ? 256 : 128));
-    const int a_rows = pl.pair ? p.bn / 2 : p.bn;
-    p.stages = std::min(IM_MAX_ST, (int)((IM_SMEM - 1024) / (CHUNK_BYTES + (size_t)a_rows * 128)));
-    p.a_scale = a_scale; p.b_scale = b_scale; p.out = out; p.ldo = ldo; p.dev_status = dev_status;
-    CUtensorMap ma, mb;
-    if (!make_map_i8(&ma, A, rows, k, lda, a_rows) || !make_map_i8(&mb, B, cols, k, ldb, 128)) return GC_ERR_CUDA;
-    using Kernel = void (*)(CUtensorMap, CUtensorMap, ImParams);
-    static const Kernel kernels[4] = {matmul_i8_kernel<false, false>, matmul_i8_kernel<false, true>,
-                                      matmul_i8_kernel<true, false>, matmul_i8_kernel<true, true>};
+    p.tiles_m = (int)((p.rows_m + (pl.pair ? 255 : 127)) / (pl.pair ? 256 : 128));
+    p.tiles_n = (int)((p.rows_n + p.bn - 1) / p.bn);
+    const int n_rows = pl.pair ? p.bn / 2 : p.bn;
+    const size_t room = IM_SMEM - 1024 - (pl.staged ? NSOFT * (2 * 4096 + 512) : 0);
+    p.stages = std::min(IM_MAX_ST, (int)(room / (CHUNK_BYTES + (size_t)n_rows * 128)));
+    p.out = out; p.ldo = ldo; p.dev_status = dev_status;
+    p.whole = cols & ~(int64_t)(bf16 ? 7 : 3);
+    CUtensorMap mm, mn, mo;
+    if (!make_map_i8(&mm, pl.staged ? A : B, p.rows_m, k, pl.staged ? lda : ldb, 128) ||
+        !make_map_i8(&mn, pl.staged ? B : A, p.rows_n, k, pl.staged ? ldb : lda, n_rows) ||
+        !(pl.staged ? make_map_out(&mo, out, rows, p.whole, ldo, bf16) : (mo = mm, true)))
+        return GC_ERR_CUDA;
+    using Kernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, ImParams);
+    static const Kernel kernels[8] = {
+        matmul_i8_kernel<false, false, false>, matmul_i8_kernel<false, true, false>,
+        matmul_i8_kernel<true, false, false>, matmul_i8_kernel<true, true, false>,
+        matmul_i8_kernel<false, false, true>, matmul_i8_kernel<false, true, true>,
+        matmul_i8_kernel<true, false, true>, matmul_i8_kernel<true, true, true>};
     static bool configured_on[64] = {false};       // the attribute belongs to (kernel, device)
     if (!configured_on[dev]) {
         for (const Kernel kernel : kernels)
@@ -597,10 +770,10 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
             }
         configured_on[dev] = true;
     }
-    const int64_t total = (int64_t)p.tiles_a * p.tiles_b, units = sm_count() / (pl.pair ? 2 : 1);
+    const int64_t total = (int64_t)p.tiles_m * p.tiles_n, units = sm_count() / (pl.pair ? 2 : 1);
     const dim3 grid((unsigned)std::min(total, units) * (pl.pair ? 2u : 1u));
-    const cudaError_t e = launch_chained(kernels[2 * pl.pair + (out_dtype == GC_BF16)], grid, NTHREADS, IM_SMEM,
-                                         pl.pair ? 2 : 1, static_cast<cudaStream_t>(cuda_stream), ma, mb, p);
+    const cudaError_t e = launch_chained(kernels[4 * pl.staged + 2 * pl.pair + bf16], grid, NTHREADS, IM_SMEM,
+                                         pl.pair ? 2 : 1, static_cast<cudaStream_t>(cuda_stream), mm, mn, mo, p);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return GC_ERR_CUDA;
