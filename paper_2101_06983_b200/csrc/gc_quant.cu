@@ -203,6 +203,9 @@ quantize_rows_kernel(const void* X, int64_t ldx, int64_t rows, int64_t d, int8_t
 constexpr int IM_KB = 128;                 // contraction depth of a ring stage: one swizzle row of bytes
 constexpr int IM_MAX_ST = 11;
 constexpr size_t IM_SMEM = 225 * 1024;
+constexpr int IM_EPI = 16;                 // epilogue warps: four to a quarter of the lanes
+constexpr int IM_THREADS = 32 * (NPROD + 1 + IM_EPI);
+constexpr uint32_t IM_SCALES = 256;        // bytes of a warp: the scales of its 64 columns
 
 // The product as the tensor cores see it: rows of the M side (128 to a CTA) are lanes of tensor memory, rows of the
 // N side (bn to a tile) its columns.
@@ -259,14 +262,28 @@ __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint32_t a_lo, uint32_t 
     }
 }
 
-// Not staged: one block of G rows of A x this warp's 32 rows of B: v the sums (column e: row of A), sa the scale of
-// row `lane` of the block.  Stores `n` of the G rows, the first at `row`.
-template <int G, bool BF16>
-__device__ __forceinline__ void store_block(const uint32_t (&v)[G], float sa, float sb, const ImParams& p, int64_t row,
-                                            int n, int64_t j, int lane) {
-    float f[G];
+// The products of 32 lanes' sums with the scales of the N side's rows (in shared memory) and of the lane's row; the
+// order is a_scale first.
+template <int G, bool LANE_FIRST>
+__device__ __forceinline__ void scale_sums(const uint32_t (&v)[G], uint32_t scales, float lane_scale, float (&f)[G]) {
+    const uint64_t mine = pack2(lane_scale, lane_scale);
 #pragma unroll
-    for (int e = 0; e < G; ++e) f[e] = (float)(int)v[e] * __shfl_sync(0xffffffffu, sa, e) * sb;
+    for (int e = 0; e < G; e += 4) {
+        uint64_t s0, s1;
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(s0), "=l"(s1) : "r"(scales + 4 * e));
+        const uint64_t x = pack2((float)(int)v[e], (float)(int)v[e + 1]);
+        const uint64_t y = pack2((float)(int)v[e + 2], (float)(int)v[e + 3]);
+        unpack2(LANE_FIRST ? mul2(mul2(x, mine), s0) : mul2(mul2(x, s0), mine), f[e], f[e + 1]);
+        unpack2(LANE_FIRST ? mul2(mul2(y, mine), s1) : mul2(mul2(y, s1), mine), f[e + 2], f[e + 3]);
+    }
+}
+// Not staged: one block of G rows of A x this warp's 32 rows of B: v the sums (column e: row of A), `scales` those
+// rows' scales.  Stores `n` of the G rows, the first at `row`.
+template <int G, bool BF16>
+__device__ __forceinline__ void store_block(const uint32_t (&v)[G], uint32_t scales, float sb, const ImParams& p,
+                                            int64_t row, int n, int64_t j, int lane) {
+    float f[G];
+    scale_sums<G, false>(v, scales, sb, f);
     if (BF16) {
         // neighbouring lanes trade a row, so that a lane stores two neighbouring outputs
         const int odd = lane & 1;
@@ -283,9 +300,15 @@ __device__ __forceinline__ void store_block(const uint32_t (&v)[G], float sa, fl
             }
             dst += 2 * p.ldo;
         }
-    } else {
+    } else if (j < p.rows_m) {
         float* dst = static_cast<float*>(p.out) + row * p.ldo + j;
-        if (j < p.rows_m) {
+        if (n >= G) {
+#pragma unroll
+            for (int e = 0; e < G; ++e) {
+                *dst = f[e];
+                dst += p.ldo;
+            }
+        } else {
 #pragma unroll
             for (int e = 0; e < G; ++e) {
                 if (e < n) *dst = f[e];
@@ -298,7 +321,7 @@ __device__ __forceinline__ void store_block(const uint32_t (&v)[G], float sa, fl
 // PAIR: a cluster of two CTAs owns 256 rows of the M side x bn of the N side, 128 and half of bn loaded by each CTA,
 // which holds the accumulators of its 128; otherwise a CTA owns 128 x bn.
 template <bool PAIR, bool BF16, bool STAGED>
-__global__ void __launch_bounds__(NTHREADS, 1)
+__global__ void __launch_bounds__(IM_THREADS, 1)
 matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant__ CUtensorMap mapN,
                  const __grid_constant__ CUtensorMap mapO, const ImParams p) {
     extern __shared__ uint8_t smem_raw[];
@@ -320,7 +343,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&bars.acc_full[b]), 1);
-            mbar_init(smem_u32(&bars.acc_free[b]), NSOFT);
+            mbar_init(smem_u32(&bars.acc_free[b]), IM_EPI);
             mbar_init(smem_u32(&bars.acc_free_peer[b]), 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -429,61 +452,66 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
                 if (ok && elect_one()) mbar_arrive_cluster(mapa_u32(smem_u32(&bars.acc_free_peer[use & 1]), 0));
             }
         }
-    } else if (STAGED) {
-        // warp: 32 rows of A (a quarter of the lanes), every other block of WIDE columns (128 bytes of output)
-        constexpr int WIDE = BF16 ? 64 : 32, BLOCKS = 256 / WIDE / 2;
-        const int q = warp & 3, ew = warp - (NPROD + 1), half = ew >> 2;
-        const uint32_t slot = smem + p.stages * stage_bytes + (uint32_t)ew * (2 * 4096u);
-        const uint32_t scales = smem + p.stages * stage_bytes + NSOFT * 2 * 4096u + (uint32_t)ew * 512u;
-        int use = 0, sent = 0;
+    } else {
+        // A warp has 32 rows of the M side (a quarter of the lanes) and every fourth block of columns: 128 bytes of
+        // output where they are staged, else 32 (16 in small tiles).
+        const int q = warp & 3, ew = warp - (NPROD + 1), group = ew >> 2;
+        const int block = STAGED ? (BF16 ? 64 : 32) : p.bn >= 64 ? 32 : 16;
+        const uint32_t after = smem + p.stages * stage_bytes;
+        const uint32_t scales = after + (uint32_t)ew * IM_SCALES, buf = after + IM_EPI * IM_SCALES + (uint32_t)ew * 4096u;
+        float next_m = 0.f, next_n[2] = {0.f, 0.f};
+        // the scales of a tile's rows and of this warp's columns of it, block after block
+        auto fetch = [&](int64_t t) {
+            if (t >= total) return;
+            int tm, tn;
+            tile_at(t, &tm, &tn);
+            const int64_t i = (int64_t)tm * M_ROWS + rank * 128 + 32 * q + lane, j0 = (int64_t)tn * p.bn;
+            const int n = (int)min((int64_t)p.bn, p.rows_n - j0);
+            next_m = i < p.rows_m ? p.m_scale[i] : 0.f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int c = 32 * x + lane, col = (4 * (c / block) + group) * block + c % block;
+                next_n[x] = col < n ? p.n_scale[j0 + col] : 0.f;
+            }
+        };
+        fetch(first);
+        int use = 0;
         for (int64_t t = first; t < total; t += by, ++use) {
             int tm, tn;
             tile_at(t, &tm, &tn);
-            const int64_t row0 = (int64_t)tm * M_ROWS + rank * 128 + 32 * q, i = row0 + lane;
+            const int64_t row0 = (int64_t)tm * M_ROWS + rank * 128 + 32 * q, i = row0 + lane;   // the lane's row
             const int64_t j0 = (int64_t)tn * p.bn;
             const int n = (int)min((int64_t)p.bn, p.rows_n - j0);
-            const float sa = i < p.rows_m ? p.m_scale[i] : 0.f;
-            // the scales of this warp's columns, block after block
+            const float mine = next_m;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int c = 32 * x + lane, col = (2 * (c / WIDE) + half) * WIDE + c % WIDE;
-                const float sb = col < n ? p.n_scale[j0 + col] : 0.f;
-                asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + 4 * c), "f"(sb) : "memory");
-            }
+            for (int x = 0; x < 2; ++x)
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + 4 * (32 * x + lane)), "f"(next_n[x]) : "memory");
             __syncwarp();
+            fetch(t + by);
             if (!mbar_wait(smem_u32(&bars.acc_full[use & 1]), (uint32_t)(use >> 1) & 1u, abort_flag)) break;
             tc_fence_after();
             const uint32_t src = tmem + (use & 1) * 256 + ((uint32_t)(32 * q) << 16);
             if (row0 < p.rows_m) {
+                if (STAGED) {
 #pragma unroll 1
-                for (int x = 0; x < BLOCKS; ++x) {
-                    const int c = (2 * x + half) * WIDE;
-                    if (c >= n) break;
-                    const uint32_t buf = slot + (uint32_t)(sent & 1) * 4096u;
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                    __syncwarp();
-#pragma unroll
-                    for (int h = 0; h < WIDE / 32; ++h) {
+                    for (int y = 0; y < 2; ++y) {                            // 32 columns each
+                        const int part = BF16 ? y : 0;                       // of a block of 128 bytes
+                        const int c = BF16 ? group * 64 + 32 * y : (4 * y + group) * 32;
+                        if (c - 32 * part >= n) break;
                         uint32_t v[32];
-                        tmem_ld32(src + c + 32 * h, v);
+                        tmem_ld32(src + c, v);
+                        if (part == 0) {
+                            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                            __syncwarp();
+                        }
                         tmem_ld_wait();
                         float f[32];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            float s0, s1, s2, s3;
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                         : "=f"(s0), "=f"(s1), "=f"(s2), "=f"(s3)
-                                         : "r"(scales + 4 * (x * WIDE + 32 * h + e)));
-                            f[e] = (float)(int)v[e] * sa * s0;
-                            f[e + 1] = (float)(int)v[e + 1] * sa * s1;
-                            f[e + 2] = (float)(int)v[e + 2] * sa * s2;
-                            f[e + 3] = (float)(int)v[e + 3] * sa * s3;
-                        }
-                        if (j0 + c + 32 * h + 32 > p.whole && p.whole < p.rows_n && i < p.rows_m) {
+                        scale_sums<32, true>(v, scales + 128 * y, mine, f);
+                        if (j0 + c + 32 > p.whole && p.whole < p.rows_n && i < p.rows_m) {
                             // the columns after the last whole 16 bytes
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
-                                const int64_t j = j0 + c + 32 * h + e;
+                                const int64_t j = j0 + c + e;
                                 if (j >= p.whole && j < p.rows_n) {
                                     if (BF16) static_cast<__nv_bfloat16*>(p.out)[i * p.ldo + j] = __float2bfloat16_rn(f[e]);
                                     else      static_cast<float*>(p.out)[i * p.ldo + j] = f[e];
@@ -495,83 +523,50 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
                         for (int k = 0; k < (BF16 ? 4 : 8); ++k) {
                             uint32_t w[4];
 #pragma unroll
-                            for (int y = 0; y < 4; ++y) {
+                            for (int z = 0; z < 4; ++z) {
                                 if (BF16) {
-                                    const __nv_bfloat162 b = __floats2bfloat162_rn(f[8 * (k & 3) + 2 * y],
-                                                                                   f[8 * (k & 3) + 2 * y + 1]);
-                                    w[y] = *reinterpret_cast<const uint32_t*>(&b);
+                                    const __nv_bfloat162 h = __floats2bfloat162_rn(f[8 * (k & 3) + 2 * z],
+                                                                                   f[8 * (k & 3) + 2 * z + 1]);
+                                    w[z] = *reinterpret_cast<const uint32_t*>(&h);
                                 } else {
-                                    w[y] = __float_as_uint(f[4 * k + y]);
+                                    w[z] = __float_as_uint(f[4 * k + z]);
                                 }
                             }
-                            const uint32_t at = buf + lane * 128 + (((4 * (BF16 ? h : 0) + k) ^ (lane & 7)) << 4);
+                            const uint32_t at = buf + lane * 128 + (((4 * part + k) ^ (lane & 7)) << 4);
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
                                          ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
                         }
+                        if (!BF16 || part == 1) {
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                            __syncwarp();
+                            const int64_t at = j0 + c - 32 * part;
+                            if (lane == 0 && at < p.whole) tma_store_2d(&mapO, buf, (int)at, (int)row0);
+                        }
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (j0 + c < p.whole) {
-                        if (lane == 0) tma_store_2d(&mapO, buf, (int)(j0 + c), (int)row0);
-                        ++sent;
+                } else if (block == 32) {
+#pragma unroll 1
+                    for (int y = 0; y < 2; ++y) {
+                        const int c = (4 * y + group) * 32;
+                        if (c >= n) break;
+                        uint32_t v[32];
+                        tmem_ld32(src + c, v);
+                        tmem_ld_wait();
+                        store_block<32, BF16>(v, scales + 128 * y, mine, p, j0 + c, n - c, i, lane);
                     }
+                } else if (group * 16 < n) {
+                    uint32_t v[16];
+                    tmem_ld16(src + group * 16, v);
+                    tmem_ld_wait();
+                    store_block<16, BF16>(v, scales, mine, p, j0 + group * 16, n - group * 16, i, lane);
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars.acc_free[use & 1]));
         }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        __syncwarp();
-    } else {
-        // warp: 32 rows of B (a quarter of the lanes), every other block of 32 rows of A (16 in small tiles)
-        const int q = warp & 3, half = (warp - (NPROD + 1)) >> 2;
-        const int block = p.bn >= 64 ? 32 : 16;
-        int use = 0;
-        for (int64_t t = first; t < total; t += by, ++use) {
-            int tm, tn;
-            tile_at(t, &tm, &tn);
-            const int64_t row0 = (int64_t)tm * M_ROWS + rank * 128 + 32 * q, j = row0 + lane;   // this lane's row of B
-            const int64_t i0 = (int64_t)tn * p.bn;
-            const int n = (int)min((int64_t)p.bn, p.rows_n - i0);
-            const float sb = j < p.rows_m ? p.m_scale[j] : 0.f;
-            float sa[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int c = (2 * x + half) * block + lane;
-                sa[x] = c < n ? p.n_scale[i0 + c] : 0.f;
-            }
-            if (!mbar_wait(smem_u32(&bars.acc_full[use & 1]), (uint32_t)(use >> 1) & 1u, abort_flag)) break;
-            tc_fence_after();
-            const uint32_t src = tmem + (use & 1) * 256 + ((uint32_t)(32 * q) << 16);
-            if (row0 < p.rows_m) {
-                if (block == 32) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int c = (2 * x + half) * 32;
-                        if (c < n) {
-                            uint32_t v[32];
-                            tmem_ld32(src + c, v);
-                            tmem_ld_wait();
-                            store_block<32, BF16>(v, sa[x], sb, p, i0 + c, n - c, j, lane);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int c = (2 * x + half) * 16;
-                        if (c < n) {
-                            uint32_t v[16];
-                            tmem_ld16(src + c, v);
-                            tmem_ld_wait();
-                            store_block<16, BF16>(v, sa[x], sb, p, i0 + c, n - c, j, lane);
-                        }
-                    }
-                }
-            }
-            tc_fence_before();
+        if (STAGED) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars.acc_free[use & 1]));
         }
     }
 
@@ -746,7 +741,7 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     p.tiles_m = (int)((p.rows_m + (pl.pair ? 255 : 127)) / (pl.pair ? 256 : 128));
     p.tiles_n = (int)((p.rows_n + p.bn - 1) / p.bn);
     const int n_rows = pl.pair ? p.bn / 2 : p.bn;
-    const size_t room = IM_SMEM - 1024 - (pl.staged ? NSOFT * (2 * 4096 + 512) : 0);
+    const size_t room = IM_SMEM - 1024 - IM_EPI * (IM_SCALES + (pl.staged ? 4096 : 0));
     p.stages = std::min(IM_MAX_ST, (int)(room / (CHUNK_BYTES + (size_t)n_rows * 128)));
     p.out = out; p.ldo = ldo; p.dev_status = dev_status;
     p.whole = cols & ~(int64_t)(bf16 ? 7 : 3);
@@ -772,7 +767,7 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     }
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n, units = sm_count() / (pl.pair ? 2 : 1);
     const dim3 grid((unsigned)std::min(total, units) * (pl.pair ? 2u : 1u));
-    const cudaError_t e = launch_chained(kernels[4 * pl.staged + 2 * pl.pair + bf16], grid, NTHREADS, IM_SMEM,
+    const cudaError_t e = launch_chained(kernels[4 * pl.staged + 2 * pl.pair + bf16], grid, IM_THREADS, IM_SMEM,
                                          pl.pair ? 2 : 1, static_cast<cudaStream_t>(cuda_stream), mm, mn, mo, p);
     if (e != cudaSuccess) {
         cudaGetLastError();
