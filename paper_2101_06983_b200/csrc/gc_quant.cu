@@ -128,7 +128,7 @@ __device__ __forceinline__ float reciprocal(float s, float amax) {
 template <bool BF16, int LANES, int KEEP>
 __global__ void __launch_bounds__(QZ_THREADS, QZ_BLOCKS)
 quantize_rows_kernel(const void* X, int64_t ldx, int64_t rows, int64_t d, int8_t* q, int64_t ldq, float* scale) {
-    constexpr int PER_BLOCK = QZ_THREADS / LANES, STEP = LANES * 8, WARPS = LANES / 32;
+    constexpr int PER_BLOCK = QZ_THREADS / LANES, STEP = LANES * 8, WARPS = LANES < 32 ? 1 : LANES / 32;
     __shared__ uint32_t warp_max[2][QZ_THREADS / 32];
     const int lane = threadIdx.x % LANES, warp = threadIdx.x >> 5;
     const int64_t k0 = 8 * lane, pitch = ldx * (BF16 ? 2 : 4);
@@ -209,10 +209,11 @@ constexpr uint32_t IM_SCALES = 256;        // bytes of a warp: the scales of its
 
 // The product as the tensor cores see it: rows of the M side (128 to a CTA) are lanes of tensor memory, rows of the
 // N side (bn to a tile) its columns.
-//   staged     M: A (tokens), N: B (channels).  A lane holds neighbouring outputs of a row; blocks of 32 rows x 128 bytes
-//              leave through shared memory with bulk tensor stores.
-//   otherwise  M: B, N: A.  32 lanes hold neighbouring outputs and store them as they are: for few rows of A, which
-//              cost no more than their share of the instruction.
+//   plain      M: B (channels), N: A (tokens).  32 lanes hold neighbouring outputs and store them as they are.  Few rows
+//              of A cost no more than their share of the instruction.
+//   staged     bf16 outputs only.  M: A, N: B.  A lane holds neighbouring outputs of a row; blocks of 32 rows x 64
+//              columns leave through shared memory with bulk tensor stores: half the words to shared memory that
+//              fp32 would take, and no trading of rows between lanes.
 struct ImParams {
     int64_t rows_m, rows_n;
     int kblocks;
@@ -324,6 +325,7 @@ template <bool PAIR, bool BF16, bool STAGED>
 __global__ void __launch_bounds__(IM_THREADS, 1)
 matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant__ CUtensorMap mapN,
                  const __grid_constant__ CUtensorMap mapO, const ImParams p) {
+    static_assert(BF16 || !STAGED, "fp32 outputs are stored as they are");
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) ImBars bars;
     __shared__ uint32_t tmem_s;
@@ -453,10 +455,10 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
             }
         }
     } else {
-        // A warp has 32 rows of the M side (a quarter of the lanes) and every fourth block of columns: 128 bytes of
-        // output where they are staged, else 32 (16 in small tiles).
+        // A warp has 32 rows of the M side (a quarter of the lanes) and every fourth block of columns: 64 where they are
+        // staged, else 32 (16 in small tiles).
         const int q = warp & 3, ew = warp - (NPROD + 1), group = ew >> 2;
-        const int block = STAGED ? (BF16 ? 64 : 32) : p.bn >= 64 ? 32 : 16;
+        const int block = STAGED ? 64 : p.bn >= 64 ? 32 : 16;
         const uint32_t after = smem + p.stages * stage_bytes;
         const uint32_t scales = after + (uint32_t)ew * IM_SCALES, buf = after + IM_EPI * IM_SCALES + (uint32_t)ew * 4096u;
         float next_m = 0.f, next_n[2] = {0.f, 0.f};
@@ -493,14 +495,13 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
             const uint32_t src = tmem + (use & 1) * 256 + ((uint32_t)(32 * q) << 16);
             if (row0 < p.rows_m) {
                 if (STAGED) {
+                    const int c0 = group * 64;
 #pragma unroll 1
-                    for (int y = 0; y < 2; ++y) {                            // 32 columns each
-                        const int part = BF16 ? y : 0;                       // of a block of 128 bytes
-                        const int c = BF16 ? group * 64 + 32 * y : (4 * y + group) * 32;
-                        if (c - 32 * part >= n) break;
+                    for (int y = 0; y < 2 && c0 < n; ++y) {                  // 32 columns each
+                        const int c = c0 + 32 * y;
                         uint32_t v[32];
                         tmem_ld32(src + c, v);
-                        if (part == 0) {
+                        if (y == 0) {
                             if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                             __syncwarp();
                         }
@@ -512,35 +513,27 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
                                 const int64_t j = j0 + c + e;
-                                if (j >= p.whole && j < p.rows_n) {
-                                    if (BF16) static_cast<__nv_bfloat16*>(p.out)[i * p.ldo + j] = __float2bfloat16_rn(f[e]);
-                                    else      static_cast<float*>(p.out)[i * p.ldo + j] = f[e];
-                                }
+                                if (j >= p.whole && j < p.rows_n)
+                                    static_cast<__nv_bfloat16*>(p.out)[i * p.ldo + j] = __float2bfloat16_rn(f[e]);
                             }
                         }
                         // 16-byte chunk k of row r lies at chunk k ^ (r & 7): the map's 128-byte swizzle
 #pragma unroll
-                        for (int k = 0; k < (BF16 ? 4 : 8); ++k) {
+                        for (int k = 0; k < 4; ++k) {
                             uint32_t w[4];
 #pragma unroll
                             for (int z = 0; z < 4; ++z) {
-                                if (BF16) {
-                                    const __nv_bfloat162 h = __floats2bfloat162_rn(f[8 * (k & 3) + 2 * z],
-                                                                                   f[8 * (k & 3) + 2 * z + 1]);
-                                    w[z] = *reinterpret_cast<const uint32_t*>(&h);
-                                } else {
-                                    w[z] = __float_as_uint(f[4 * k + z]);
-                                }
+                                const __nv_bfloat162 h = __floats2bfloat162_rn(f[8 * k + 2 * z], f[8 * k + 2 * z + 1]);
+                                w[z] = *reinterpret_cast<const uint32_t*>(&h);
                             }
-                            const uint32_t at = buf + lane * 128 + (((4 * part + k) ^ (lane & 7)) << 4);
+                            const uint32_t at = buf + lane * 128 + (((4 * y + k) ^ (lane & 7)) << 4);
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
                                          ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
                         }
-                        if (!BF16 || part == 1) {
+                        if (y == 1) {
                             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                             __syncwarp();
-                            const int64_t at = j0 + c - 32 * part;
-                            if (lane == 0 && at < p.whole) tma_store_2d(&mapO, buf, (int)at, (int)row0);
+                            if (lane == 0 && j0 + c0 < p.whole) tma_store_2d(&mapO, buf, (int)(j0 + c0), (int)row0);
                         }
                     }
                 } else if (block == 32) {
@@ -624,26 +617,29 @@ int check_device(int* dev) {
     return *dev < 0 || *dev >= 64 ? GC_ERR_CUDA : GC_OK;
 }
 
-// Row-major output of whole 16 bytes, boxes of 32 rows x 128 bytes, 128-byte swizzle; what lies past the ends is
+// Row-major bf16 output of whole 16 bytes, boxes of 32 rows x 128 bytes, 128-byte swizzle; what lies past the ends is
 // not written.
-bool make_map_out(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t ld, bool bf16) {
+bool make_map_out(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t ld) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)ld * (bf16 ? 2 : 4)};
-    cuuint32_t box[2] = {bf16 ? 64u : 32u, 32};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    cuuint32_t box[2] = {64, 32};
     cuuint32_t estr[2] = {1, 1};
-    return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides,
-              box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+           CUDA_SUCCESS;
 }
 
 struct ImPlan { bool pair, staged; int bn; };
 
-// The tile that costs least by a count of cycles: rounds of tiles, each its products, its loads (85 bytes a
-// cycle) or its stores, whichever is longest, and the stores of the last one.
-ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, int out_dtype) {
+// The tile that costs least by a count of cycles: rounds of tiles, each its products or loads, whichever is longer, or
+// its stores where they are longer still, and the stores of the last one.  The constants are fitted to 72 shapes with every
+// choice forced, one row to 60000 and contractions of 40 to 8192: 2 % behind the best choice on average, 14 % at
+// most.  bf16 outputs without staging would be 7 % behind (69 % at most), all of them staged 6 (60).
+ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, bool bf16) {
     ImPlan best{false, false, 16};
+    double least = INFINITY;
 #ifdef IM_TUNE
     if (getenv("IM_PLAN")) {
         int a, b, c;
@@ -651,21 +647,19 @@ ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, int out_dtype) {
         return ImPlan{a != 0, b != 0, c};
     }
 #endif
-    double least = INFINITY;
     const double kblocks = (double)((k + IM_KB - 1) / IM_KB);
-    for (int staged = 0; staged < (cols >= 8 ? 2 : 1); ++staged) {
+    for (int staged = 0; staged < (bf16 && cols >= 8 ? 2 : 1); ++staged) {
         const int64_t m = staged ? rows : cols, n = staged ? cols : rows;
         for (int pair = 0; pair < 2; ++pair)
-            // (a staged block of 128 bytes must not reach into the next tile)
-            for (int step = staged ? (out_dtype == GC_BF16 ? 64 : 32) : pair ? 32 : 16, bn = step;
-                 bn <= 256 && bn < n + step; bn += step) {
+            // (a staged block of 64 columns must not reach into the next tile)
+            for (int step = staged ? 64 : pair ? 32 : 16, bn = step; bn <= 256 && bn < n + step; bn += step) {
                 const int64_t tn = (n + bn - 1) / bn, tm = (m + (pair ? 255 : 127)) / (pair ? 256 : 128);
                 const int64_t units = sm_count() / (pair ? 2 : 1);
                 const double rounds = (double)((tm * tn + units - 1) / units);
-                const double products = pair ? std::max(2.0 * bn, 190.0) : 4 * (bn / 2.0 + 44);
-                const double loads = (CHUNK_BYTES + 128.0 * (pair ? bn / 2 : bn)) / 85;
-                const double stores = 128.0 * bn * (out_dtype == GC_BF16 ? 2 : 4) / (staged ? 25 : 10);
-                const double cost = rounds * std::max(kblocks * std::max(products, loads), stores) + stores;
+                const double products = pair ? 2.0 * bn : 2.0 * bn + 336;
+                const double loads = (CHUNK_BYTES + 128.0 * (pair ? bn / 2 : bn)) / 59;
+                const double stores = 800 + 128.0 * bn * (bf16 ? 2.0 / (staged ? 53 : 18) : 4.0 / 65);
+                const double cost = rounds * std::max(kblocks * std::max(products, loads) + 500, stores) + 1.33 * stores;
                 if (cost < least) {
                     least = cost;
                     best = {pair != 0, staged != 0, bn};
@@ -729,8 +723,8 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     if (k > 131071) return GC_ERR_LIMIT;           // 2^14 (k of -128 times -128) must fit 31 bits
     int dev;
     if ((rc = check_device(&dev))) return rc;
-    const ImPlan pl = make_im_plan(rows, cols, k, out_dtype);
     const bool bf16 = out_dtype == GC_BF16;
+    const ImPlan pl = make_im_plan(rows, cols, k, bf16);
     ImParams p{};
     p.rows_m = pl.staged ? rows : cols;
     p.rows_n = pl.staged ? cols : rows;
@@ -744,18 +738,17 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     const size_t room = IM_SMEM - 1024 - IM_EPI * (IM_SCALES + (pl.staged ? 4096 : 0));
     p.stages = std::min(IM_MAX_ST, (int)(room / (CHUNK_BYTES + (size_t)n_rows * 128)));
     p.out = out; p.ldo = ldo; p.dev_status = dev_status;
-    p.whole = cols & ~(int64_t)(bf16 ? 7 : 3);
+    p.whole = cols & ~(int64_t)7;
     CUtensorMap mm, mn, mo;
     if (!make_map_i8(&mm, pl.staged ? A : B, p.rows_m, k, pl.staged ? lda : ldb, 128) ||
         !make_map_i8(&mn, pl.staged ? B : A, p.rows_n, k, pl.staged ? ldb : lda, n_rows) ||
-        !(pl.staged ? make_map_out(&mo, out, rows, p.whole, ldo, bf16) : (mo = mm, true)))
+        !(pl.staged ? make_map_out(&mo, out, rows, p.whole, ldo) : (mo = mm, true)))
         return GC_ERR_CUDA;
     using Kernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, ImParams);
-    static const Kernel kernels[8] = {
-        matmul_i8_kernel<false, false, false>, matmul_i8_kernel<false, true, false>,
-        matmul_i8_kernel<true, false, false>, matmul_i8_kernel<true, true, false>,
-        matmul_i8_kernel<false, false, true>, matmul_i8_kernel<false, true, true>,
-        matmul_i8_kernel<true, false, true>, matmul_i8_kernel<true, true, true>};
+    static const Kernel kernels[6] = {
+        matmul_i8_kernel<false, false, false>, matmul_i8_kernel<true, false, false>,
+        matmul_i8_kernel<false, true, false>, matmul_i8_kernel<true, true, false>,
+        matmul_i8_kernel<false, true, true>, matmul_i8_kernel<true, true, true>};
     static bool configured_on[64] = {false};       // the attribute belongs to (kernel, device)
     if (!configured_on[dev]) {
         for (const Kernel kernel : kernels)
@@ -767,7 +760,7 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     }
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n, units = sm_count() / (pl.pair ? 2 : 1);
     const dim3 grid((unsigned)std::min(total, units) * (pl.pair ? 2u : 1u));
-    const cudaError_t e = launch_chained(kernels[4 * pl.staged + 2 * pl.pair + bf16], grid, IM_THREADS, IM_SMEM,
+    const cudaError_t e = launch_chained(kernels[2 * bf16 + 2 * pl.staged + pl.pair], grid, IM_THREADS, IM_SMEM,
                                          pl.pair ? 2 : 1, static_cast<cudaStream_t>(cuda_stream), mm, mn, mo, p);
     if (e != cudaSuccess) {
         cudaGetLastError();
