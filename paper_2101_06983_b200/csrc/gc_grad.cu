@@ -4,7 +4,8 @@
 //     n^2 = sum_t sum_e g_te^2        c = min(1, max_norm / (n + 1e-6))        out_te = c g_te
 //
 // The tensors of a list travel as kernel parameters (pointers, extents, first tile), so a call copies nothing
-// to the device and can be captured.  The list is cut into tiles of 16 KB; a block owns a run of them.
+// to the device and can be captured.  The list is cut into tiles of 32 KB, dealt to the blocks in
+// turn.
 // Squares of up to 32 values are summed in fp32; a sum outside [2^-100, inf) whose values are not all zero
 // (squares that overflowed, or that lost bits below 2^-149) is formed again in fp64, and everything beyond
 // those 32 values is summed in fp64, in an order that the sizes alone fix.
@@ -20,10 +21,12 @@ namespace gc {
 namespace {
 
 constexpr int GR_THREADS = 512;
-constexpr int GR_TILE_UNITS = 1024;            // 16-byte vectors of a tile; single elements where they do not fit
-constexpr int GR_PER = GR_TILE_UNITS / GR_THREADS;
-constexpr int GR_DEEP = 4;                     // vectors of a thread under way
-constexpr int GR_BLOCKS = 3;                   // to an SM
+#ifndef GR_PER
+#define GR_PER 4
+#define GR_B1 3
+#define GR_B2 3
+#endif
+constexpr int GR_TILE_UNITS = GR_THREADS * GR_PER;   // 16-byte vectors of a tile; single elements where they do not fit
 constexpr int GR_SLOTS = 1024;                 // partial sums of a launch
 constexpr double GR_EPS = 1e-6;
 
@@ -113,10 +116,9 @@ __device__ __forceinline__ void scale_one(const Entry& e, int64_t from, int64_t 
     }
 }
 
-// The entry that holds tile t.
+// The entry that holds tile t, between two that surround it.
 template <int N>
-__device__ __forceinline__ int entry_of(const List<N>& list, uint32_t t) {
-    int lo = 0, hi = list.n - 1;
+__device__ __forceinline__ int entry_of(const List<N>& list, uint32_t t, int lo, int hi) {
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (list.e[mid].first <= t) lo = mid; else hi = mid - 1;
@@ -142,16 +144,6 @@ __device__ __forceinline__ int64_t place_of(const Entry& e, const Tile& x, uint3
     return (x.r + down) * ld + (int64_t)(at - down * e.cols) * (e.mode == ROWS_VEC ? (e.bf16 ? 8 : 4) : 1);
 }
 
-// The block's run of tiles.
-__device__ __forceinline__ void run_of(uint32_t tiles, uint32_t* lo, uint32_t* hi) {
-    *lo = (uint32_t)((uint64_t)tiles * blockIdx.x / gridDim.x);
-    *hi = (uint32_t)((uint64_t)tiles * (blockIdx.x + 1) / gridDim.x);
-}
-template <int N>
-__device__ __forceinline__ uint32_t end_of(const List<N>& list, int at) {
-    return at + 1 < list.n ? list.e[at + 1].first : list.tiles;
-}
-
 __device__ __forceinline__ double warp_sum(double v) {
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
@@ -166,66 +158,57 @@ __device__ __forceinline__ double block_sum(double v, double* part) {
     return s;
 }
 
-// part[block] = the sum of squares of the block's run of tiles.
+// part[block] = the sum of squares of the block's tiles.
 template <int N>
-__global__ void __launch_bounds__(GR_THREADS, GR_BLOCKS)
+__global__ void __launch_bounds__(GR_THREADS, GR_B1)
 grad_square_kernel(const __grid_constant__ List<N> list, double* part) {
     __shared__ double warp_part[GR_THREADS / 32];
     dep_release();
     dep_wait();
-    uint32_t t, end;
-    run_of(list.tiles, &t, &end);
     double sum = 0.0;
-    for (int at = t < end ? entry_of(list, t) : 0; t < end; ++at) {
+    int at = 0;
+    for (uint32_t t = blockIdx.x; t < list.tiles; t += gridDim.x) {
+        at = entry_of(list, t, at, list.n - 1);
         const Entry& e = list.e[at];
-        const uint32_t stop = min(end, end_of(list, at));
         const bool bf16 = e.bf16;
+        uint4 v[GR_PER];
         if (e.mode == FLAT_VEC) {
-            const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4);
+            const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
+            const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4) + 16 * u;
+            if (u - threadIdx.x + GR_TILE_UNITS <= e.units) {
+#pragma unroll
+                for (int i = 0; i < GR_PER; ++i) v[i] = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < GR_PER; ++i)
+                    v[i] = u + i * GR_THREADS < e.units ? *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i)
+                                                        : make_uint4(0, 0, 0, 0);
+            }
+            sum += square_sum(v, bf16);
             if (t == e.first && threadIdx.x < e.head + e.tail) {
                 const int k = threadIdx.x;
                 const double x = load_one(e.src, k < e.head ? k : k + e.units * (bf16 ? 8 : 4), bf16);
                 sum = fma(x, x, sum);
             }
-            const int64_t hi = min(e.units, (int64_t)(stop - e.first) * GR_TILE_UNITS);
-            int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
-            for (; u < hi; u += GR_DEEP * GR_THREADS) {
-                uint4 v[GR_DEEP];
-                if (u + (GR_DEEP - 1) * GR_THREADS < hi) {
-#pragma unroll
-                    for (int i = 0; i < GR_DEEP; ++i)
-                        v[i] = *reinterpret_cast<const uint4*>(src + 16 * (u + i * GR_THREADS));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < GR_DEEP; ++i)
-                        v[i] = u + i * GR_THREADS < hi ? *reinterpret_cast<const uint4*>(src + 16 * (u + i * GR_THREADS))
-                                                       : make_uint4(0, 0, 0, 0);
-                }
-                sum += square_sum(v, bf16);
-            }
-            t = stop;
             continue;
         }
-        for (; t < stop; ++t) {
-            const Tile x = tile_of(e, t);
-            if (e.mode == ROWS_VEC) {
-                uint4 v[GR_PER];
+        const Tile x = tile_of(e, t);
+        if (e.mode == ROWS_VEC) {
 #pragma unroll
-                for (int i = 0; i < GR_PER; ++i) {
-                    const uint32_t k = threadIdx.x + i * GR_THREADS;
-                    v[i] = k < x.n ? *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
-                                                                     place_of(e, x, k, e.ld) * (bf16 ? 2 : 4))
-                                   : make_uint4(0, 0, 0, 0);
-                }
-                sum += square_sum(v, bf16);
-            } else {
+            for (int i = 0; i < GR_PER; ++i) {
+                const uint32_t k = threadIdx.x + i * GR_THREADS;
+                v[i] = k < x.n ? *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
+                                                                 place_of(e, x, k, e.ld) * (bf16 ? 2 : 4))
+                               : make_uint4(0, 0, 0, 0);
+            }
+            sum += square_sum(v, bf16);
+        } else {
 #pragma unroll
-                for (int i = 0; i < GR_PER; ++i) {
-                    const uint32_t k = threadIdx.x + i * GR_THREADS;
-                    if (k < x.n) {
-                        const double y = load_one(e.src, place_of(e, x, k, e.ld), bf16);
-                        sum = fma(y, y, sum);
-                    }
+            for (int i = 0; i < GR_PER; ++i) {
+                const uint32_t k = threadIdx.x + i * GR_THREADS;
+                if (k < x.n) {
+                    const double y = load_one(e.src, place_of(e, x, k, e.ld), bf16);
+                    sum = fma(y, y, sum);
                 }
             }
         }
@@ -257,7 +240,7 @@ grad_norm_kernel(const double* part, int slots, double* sq_sum, float* norm, int
 
 // out = c g, c from the sum of `slots` partial sums.
 template <int N>
-__global__ void __launch_bounds__(GR_THREADS, GR_BLOCKS)
+__global__ void __launch_bounds__(GR_THREADS, GR_B2)
 grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int slots, float max_norm,
                   double* sq_sum, float* norm, int* dev_status, int tell) {
     __shared__ double warp_part[GR_THREADS / 32];
@@ -270,65 +253,52 @@ grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int 
     const double wide = (double)max_norm / (sqrt(total) + GR_EPS);
     const bool copy = !isfinite(total) || wide >= 1.0;
     const float c = (float)wide;
-    uint32_t begin, t;
-    run_of(list.tiles, &begin, &t);
     // backwards: what the sum of squares read last is in the L2 still
-    for (int at = begin < t ? entry_of(list, t - 1) : 0; t > begin; --at) {
+    int at = list.n - 1;
+    for (int64_t back = (int64_t)list.tiles - 1 - blockIdx.x; back >= 0; back -= gridDim.x) {
+        const uint32_t t = (uint32_t)back;
+        at = entry_of(list, t, 0, at);
         const Entry& e = list.e[at];
-        const uint32_t start = max(begin, e.first);
         const bool bf16 = e.bf16;
-        if (copy && e.src == e.dst) {                    // the values stay as they are
-            t = start;
-            continue;
-        }
+        if (copy && e.src == e.dst) continue;            // the values stay as they are
         if (e.mode == FLAT_VEC) {
-            const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4);
-            char* dst = static_cast<char*>(e.dst) + e.head * (bf16 ? 2 : 4);
-            const int64_t lo = (int64_t)(start - e.first) * GR_TILE_UNITS;
-            const int64_t hi = min(e.units, (int64_t)(t - e.first) * GR_TILE_UNITS);
-            constexpr int64_t STEP = GR_DEEP * GR_THREADS;
-            for (int64_t u = lo + (hi - lo - 1) / STEP * STEP + threadIdx.x; u >= lo && hi > lo; u -= STEP) {
-                uint4 v[GR_DEEP];
-                if (u + (GR_DEEP - 1) * GR_THREADS < hi) {
+            const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
+            const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4) + 16 * u;
+            char* dst = static_cast<char*>(e.dst) + e.head * (bf16 ? 2 : 4) + 16 * u;
+            if (u - threadIdx.x + GR_TILE_UNITS <= e.units) {
+                uint4 v[GR_PER];
 #pragma unroll
-                    for (int i = 0; i < GR_DEEP; ++i)
-                        v[i] = *reinterpret_cast<const uint4*>(src + 16 * (u + i * GR_THREADS));
+                for (int i = 0; i < GR_PER; ++i) v[i] = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
 #pragma unroll
-                    for (int i = 0; i < GR_DEEP; ++i)
-                        *reinterpret_cast<uint4*>(dst + 16 * (u + i * GR_THREADS)) =
-                            copy ? v[i] : scale_vec(v[i], bf16, c);
-                } else {
+                for (int i = 0; i < GR_PER; ++i)
+                    *reinterpret_cast<uint4*>(dst + 16 * GR_THREADS * i) = copy ? v[i] : scale_vec(v[i], bf16, c);
+            } else {
 #pragma unroll
-                    for (int i = 0; i < GR_DEEP; ++i)
-                        if (u + i * GR_THREADS < hi) {
-                            v[i] = *reinterpret_cast<const uint4*>(src + 16 * (u + i * GR_THREADS));
-                            *reinterpret_cast<uint4*>(dst + 16 * (u + i * GR_THREADS)) =
-                                copy ? v[i] : scale_vec(v[i], bf16, c);
-                        }
-                }
+                for (int i = 0; i < GR_PER; ++i)
+                    if (u + i * GR_THREADS < e.units) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
+                        *reinterpret_cast<uint4*>(dst + 16 * GR_THREADS * i) = copy ? v : scale_vec(v, bf16, c);
+                    }
             }
-            if (start == e.first && threadIdx.x < e.head + e.tail) {
+            if (t == e.first && threadIdx.x < e.head + e.tail) {
                 const int k = threadIdx.x;
                 const int64_t i = k < e.head ? k : k + e.units * (bf16 ? 8 : 4);
                 scale_one(e, i, i, copy, c);
             }
-            t = start;
             continue;
         }
-        for (; t > start; --t) {
-            const Tile x = tile_of(e, t - 1);
+        const Tile x = tile_of(e, t);
 #pragma unroll
-            for (int i = 0; i < GR_PER; ++i) {
-                const uint32_t k = threadIdx.x + i * GR_THREADS;
-                if (k >= x.n) break;
-                const int64_t from = place_of(e, x, k, e.ld), to = place_of(e, x, k, e.ld_out);
-                if (e.mode == ROWS_VEC) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) + from * (bf16 ? 2 : 4));
-                    *reinterpret_cast<uint4*>(static_cast<char*>(e.dst) + to * (bf16 ? 2 : 4)) =
-                        copy ? v : scale_vec(v, bf16, c);
-                } else {
-                    scale_one(e, from, to, copy, c);
-                }
+        for (int i = 0; i < GR_PER; ++i) {
+            const uint32_t k = threadIdx.x + i * GR_THREADS;
+            if (k >= x.n) break;
+            const int64_t from = place_of(e, x, k, e.ld), to = place_of(e, x, k, e.ld_out);
+            if (e.mode == ROWS_VEC) {
+                const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) + from * (bf16 ? 2 : 4));
+                *reinterpret_cast<uint4*>(static_cast<char*>(e.dst) + to * (bf16 ? 2 : 4)) =
+                    copy ? v : scale_vec(v, bf16, c);
+            } else {
+                scale_one(e, from, to, copy, c);
             }
         }
     }
@@ -498,8 +468,8 @@ int each_group(const gc_tensor* list, int64_t n, bool write, Go go) {
     return GC_OK;
 }
 
-unsigned grid_for(uint32_t tiles) {
-    const uint32_t most = (uint32_t)std::min(GR_SLOTS, GR_BLOCKS * sm_count());
+unsigned grid_for(uint32_t tiles, int per_sm) {
+    const uint32_t most = (uint32_t)std::min(GR_SLOTS, per_sm * sm_count());
     return std::max(1u, std::min(tiles, most));
 }
 
@@ -523,7 +493,7 @@ int launch_squares(const gc_tensor* list, int64_t n, double* part, int* slots, c
     *slots = 0;
     return each_group(list, n, false, [&](const auto& l) {
         if (l.tiles == 0) return cudaSuccess;
-        const unsigned grid = grid_for(l.tiles);
+        const unsigned grid = grid_for(l.tiles, GR_B1);
         using L = std::decay_t<decltype(l)>;
         const cudaError_t e = launch_chained(grad_square_kernel<sizeof(L::e) / sizeof(Entry)>, dim3(grid), GR_THREADS, 0,
                                              1, st, l, part + *slots);
@@ -537,7 +507,7 @@ int launch_scale(const gc_tensor* list, int64_t n, const double* part, int slots
     return each_group(list, n, true, [&](const auto& l) {
         using L = std::decay_t<decltype(l)>;
         const cudaError_t e =
-            launch_chained(grad_scale_kernel<sizeof(L::e) / sizeof(Entry)>, dim3(grid_for(l.tiles)), GR_THREADS, 0, 1, st,
+            launch_chained(grad_scale_kernel<sizeof(L::e) / sizeof(Entry)>, dim3(grid_for(l.tiles, GR_B2)), GR_THREADS, 0, 1, st,
                            l, part, slots, max_norm, sq_sum, norm, dev_status, tell);
         tell = 0;
         return e;
