@@ -449,15 +449,18 @@ def gc_dist_dot_block(Q, P, i0, bq, j0, bn, D_block) -> None:
         raise GradCacheError(rc, "gc_dist_dot_block")
 
 
-def _on_current_device(*tensors):
+def _on_device(dev, *tensors):
     """The library launches on the current device's current stream: refuses tensors that live elsewhere."""
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != _current_device()):
-            raise ValueError(f"tensors must be on the current CUDA device, got one on {t.device}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors must be on one CUDA device, got one on {t.device}")
+    if dev < 0 or dev != _current_device():
+        raise ValueError("tensors must be on the current CUDA device")
+    return dev
 
 
 def _scalar(t, dtype, name):
-    if t is not None and (t.dtype != dtype or t.numel() < 1):
+    if t is not None and (t.dtype is not dtype or t.numel() < 1):
         raise TypeError(f"{name} must be a {dtype} tensor of one value")
 
 
@@ -520,20 +523,16 @@ def gc_grad_workspace_bytes(n: int) -> int:
     return int(_lib.gc_grad_workspace_bytes(n))
 
 
-def _grad_args(grads, ws, scalars):
+def _grad_args(grads, ws, *others):
+    """(GradList, current device): everything lives there."""
     if not isinstance(grads, GradList):
         grads = GradList(grads)
-    if grads.device is not None and grads.device.index != _current_device():
-        raise ValueError("gradients must be on the current CUDA device")
-    _on_current_device(ws, *scalars)
-    return grads
+    dev = _current_device() if grads.device is None else grads.device.index
+    return grads, _on_device(dev, ws, *others)
 
 
-def _grad_ws(grads, ws):
-    if ws is None:
-        ws = torch.empty(gc_grad_workspace_bytes(grads.n), dtype=torch.uint8,
-                         device=torch.device("cuda", _current_device()))
-    return ws
+def _grad_ws(grads, dev):
+    return torch.empty(gc_grad_workspace_bytes(grads.n), dtype=torch.uint8, device=torch.device("cuda", dev))
 
 
 def gc_grad_norm(grads, norm=None, sq_sum=None, ws=None, dev_status=None) -> None:
@@ -541,10 +540,11 @@ def gc_grad_norm(grads, norm=None, sq_sum=None, ws=None, dev_status=None) -> Non
     (float64) its square; either may be left out.  A NaN or an infinity sets GC_DEV_GRAD_NONFINITE."""
     _scalar(norm, torch.float32, "norm")
     _scalar(sq_sum, torch.float64, "sq_sum")
-    grads = _grad_args(grads, ws, (norm, sq_sum, dev_status))
-    ws = _grad_ws(grads, ws)
-    rc = _lib.gc_grad_norm(grads.tensors, grads.n, _ptr(sq_sum), _ptr(norm), _ptr(ws), ws.numel(),
-                           _ptr(dev_status), _stream())
+    grads, dev = _grad_args(grads, ws, norm, sq_sum, dev_status)
+    if ws is None:
+        ws = _grad_ws(grads, dev)
+    rc = _lib.gc_grad_norm(grads.tensors, grads.n, _ptr(sq_sum), _ptr(norm), ws.data_ptr(), ws.numel(),
+                           _ptr(dev_status), _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_grad_norm")
 
@@ -553,9 +553,9 @@ def gc_grad_scale(grads, sq_sum, max_norm, dev_status=None) -> None:
     """Scales the gradients (in place, or into the list's `out`) by min(1, max_norm / (n + 1e-6)), with n^2 =
     sq_sum[0] (float64): of gc_grad_norm, or summed over ranks that hold different gradients."""
     _scalar(sq_sum, torch.float64, "sq_sum")
-    grads = _grad_args(grads, None, (sq_sum, dev_status))
-    rc = _lib.gc_grad_scale(grads.tensors, grads.n, _ptr(sq_sum), float(max_norm), _ptr(dev_status),
-                            _stream())
+    grads, dev = _grad_args(grads, None, sq_sum, dev_status)
+    rc = _lib.gc_grad_scale(grads.tensors, grads.n, _ptr(sq_sum), max_norm, _ptr(dev_status),
+                            _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_grad_scale")
 
@@ -566,26 +566,28 @@ def gc_grad_clip(grads, max_norm, norm, sq_sum=None, ws=None, dev_status=None) -
     finite."""
     _scalar(norm, torch.float32, "norm")
     _scalar(sq_sum, torch.float64, "sq_sum")
-    grads = _grad_args(grads, ws, (norm, sq_sum, dev_status))
-    ws = _grad_ws(grads, ws)
-    rc = _lib.gc_grad_clip(grads.tensors, grads.n, float(max_norm), _ptr(sq_sum), _ptr(norm), _ptr(ws),
-                           ws.numel(), _ptr(dev_status), _stream())
+    grads, dev = _grad_args(grads, ws, norm, sq_sum, dev_status)
+    if ws is None:
+        ws = _grad_ws(grads, dev)
+    rc = _lib.gc_grad_clip(grads.tensors, grads.n, max_norm, _ptr(sq_sum), _ptr(norm), ws.data_ptr(),
+                           ws.numel(), _ptr(dev_status), _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_grad_clip")
 
 
 def gc_quantize_rows(X, q, scale) -> None:
     """scale[i] (float32) = max |X[i]| times 1/127 and q[i] (int8) = X[i] / scale[i] to the nearest integer."""
-    if X.dim() != 2 or q.shape != X.shape or X.stride(1) != 1 or q.stride(1) != 1:
+    shape, xs, qs = X.shape, X.stride(), q.stride()
+    if len(shape) != 2 or q.shape != shape or xs[1] != 1 or qs[1] != 1:
         raise ValueError("X and q must be 2-D of one shape with unit stride along their rows")
-    rows, d = X.shape
-    if q.dtype != torch.int8 or scale.dtype != torch.float32 or not scale.is_contiguous():
+    rows, d = shape
+    if q.dtype is not torch.int8 or scale.dtype is not torch.float32 or not scale.is_contiguous():
         raise TypeError("q must be int8, scale contiguous float32")
     if scale.numel() != rows:
         raise ValueError("scale must hold one value for each row")
-    _on_current_device(X, q, scale)
-    rc = _lib.gc_quantize_rows(_ptr(X), X.stride(0), rows, d, _dtype_code(X), _ptr(q), q.stride(0),
-                               _ptr(scale), _stream())
+    dev = _on_device(X.get_device(), q, scale)
+    rc = _lib.gc_quantize_rows(X.data_ptr(), xs[0], rows, d, _dtype_code(X), q.data_ptr(), qs[0],
+                               scale.data_ptr(), _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_quantize_rows")
 
@@ -593,23 +595,21 @@ def gc_quantize_rows(X, q, scale) -> None:
 def gc_matmul_i8(A, a_scale, B, b_scale, out, dev_status=None) -> None:
     """out[i][j] = a_scale[i] b_scale[j] sum_k A[i][k] B[j][k] with A, B int8 (gc_quantize_rows), out float32 or
     bfloat16: the linear encoder's output (A inputs, B = W), or scores of queries against passages."""
-    if A.dim() != 2 or B.dim() != 2 or out.dim() != 2 or A.stride(1) != 1 or B.stride(1) != 1 \
-            or out.stride(1) != 1:
+    sa, sb, so = A.stride(), B.stride(), out.stride()
+    if len(sa) != 2 or len(sb) != 2 or len(so) != 2 or sa[1] != 1 or sb[1] != 1 or so[1] != 1:
         raise ValueError("A, B and out must be 2-D with unit stride along their rows")
     rows, k = A.shape
-    cols = B.shape[0]
-    if B.shape[1] != k or tuple(out.shape) != (rows, cols) or a_scale.numel() != rows \
-            or b_scale.numel() != cols:
+    cols, kb = B.shape
+    if kb != k or out.shape != (rows, cols) or a_scale.numel() != rows or b_scale.numel() != cols:
         raise ValueError("shape mismatch")
-    if A.dtype != torch.int8 or B.dtype != torch.int8:
+    if A.dtype is not torch.int8 or B.dtype is not torch.int8:
         raise TypeError("A and B must be int8")
     for s in (a_scale, b_scale):
-        if s.dtype != torch.float32 or not s.is_contiguous():
+        if s.dtype is not torch.float32 or not s.is_contiguous():
             raise TypeError("scales must be contiguous float32")
-    _on_current_device(A, a_scale, B, b_scale, out, dev_status)
-    rc = _lib.gc_matmul_i8(_ptr(A), A.stride(0), _ptr(a_scale), _ptr(B), B.stride(0), _ptr(b_scale), rows,
-                           cols, k, _dtype_code(out), _ptr(out), out.stride(0), _ptr(dev_status),
-                           _stream())
+    dev = _on_device(A.get_device(), a_scale, B, b_scale, out, dev_status)
+    rc = _lib.gc_matmul_i8(A.data_ptr(), sa[0], a_scale.data_ptr(), B.data_ptr(), sb[0], b_scale.data_ptr(), rows,
+                           cols, k, _dtype_code(out), out.data_ptr(), so[0], _ptr(dev_status), _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_matmul_i8")
 

@@ -21,11 +21,10 @@ namespace gc {
 namespace {
 
 constexpr int GR_THREADS = 512;
-#ifndef GR_PER
-#define GR_PER 4
-#define GR_B1 3
-#define GR_B2 3
-#endif
+constexpr int GR_PER = 4;                      // of a thread, all under way at once
+// Blocks to an SM of the two passes.  Measured, us per clipping of 357 MB fp32 / 178 MB bf16 / 666 MB bf16 with 3 and 3 blocks
+// 180 / 89 / 334, 3 and 2 177 / 88 / 332, 4 and 3 180 / 89 / 336; tiles of 16 KB 188 / 95 / 370, of 64 KB 179 / 90 / 332.
+constexpr int GR_B1 = 3, GR_B2 = 2;
 constexpr int GR_TILE_UNITS = GR_THREADS * GR_PER;   // 16-byte vectors of a tile; single elements where they do not fit
 constexpr int GR_SLOTS = 1024;                 // partial sums of a launch
 constexpr double GR_EPS = 1e-6;
@@ -49,7 +48,7 @@ struct List {
     int n;
     uint32_t tiles;
 };
-constexpr int FEW = 40, MANY = 580;            // 32,764 bytes of parameters at most
+constexpr int FEW = 32, SOME = 224, MANY = 580;        // 32,764 bytes of parameters at most; fewer are copied faster
 static_assert(sizeof(List<MANY>) <= 32600, "kernel parameters");
 
 __device__ __forceinline__ float2 widen(uint32_t w) {
@@ -429,43 +428,40 @@ int current_device() {
 
 int64_t groups_of(int64_t n) { return std::max<int64_t>(1, (n + MANY - 1) / MANY); }
 
-// go(list, tiles) for every group of at most MANY tensors in order; the group's list as a parameter.
-template <typename Go>
-int each_group(const gc_tensor* list, int64_t n, bool write, Go go) {
-    List<MANY> many;
-    int64_t i = 0;
-    do {
-        many.n = 0;
-        int64_t tiles = 0;
-        for (; i < n && many.n < MANY; ++i) {
-            if (list[i].rows == 0 || list[i].cols == 0) continue;
-            int64_t more = 0;
-            Entry e = entry_for(list[i], write, &more);
-            if (tiles + more > (int64_t)UINT32_MAX) {
-                if (many.n == 0) return GC_ERR_LIMIT;
-                break;
-            }
-            e.first = (uint32_t)tiles;
-            tiles += more;
-            many.e[many.n++] = e;
+// The next group of at most MANY tensors, from tensor *i on.
+int next_group(const gc_tensor* list, int64_t n, bool write, int64_t* i, List<MANY>& l) {
+    l.n = 0;
+    int64_t tiles = 0;
+    for (; *i < n && l.n < MANY; ++*i) {
+        if (list[*i].rows == 0 || list[*i].cols == 0) continue;
+        int64_t more = 0;
+        Entry e = entry_for(list[*i], write, &more);
+        if (tiles + more > (int64_t)UINT32_MAX) {
+            if (l.n == 0) return GC_ERR_LIMIT;
+            break;
         }
-        many.tiles = (uint32_t)tiles;
-        cudaError_t err;
-        if (many.n <= FEW) {
-            List<FEW> few;
-            std::copy(many.e, many.e + many.n, few.e);
-            few.n = many.n;
-            few.tiles = many.tiles;
-            err = go(few);
-        } else {
-            err = go(many);
-        }
-        if (err != cudaSuccess) {
-            cudaGetLastError();
-            return GC_ERR_CUDA;
-        }
-    } while (i < n);
+        e.first = (uint32_t)tiles;
+        tiles += more;
+        l.e[l.n++] = e;
+    }
+    l.tiles = (uint32_t)tiles;
     return GC_OK;
+}
+// go(list) with the smallest list type that holds the group.
+template <int N, typename Go>
+cudaError_t with_size(const List<MANY>& l, Go go) {
+    List<N> x;
+    std::copy(l.e, l.e + l.n, x.e);
+    x.n = l.n;
+    x.tiles = l.tiles;
+    return go(x);
+}
+template <typename Go>
+int with_list(const List<MANY>& l, Go go) {
+    const cudaError_t e = l.n <= FEW ? with_size<FEW>(l, go) : l.n <= SOME ? with_size<SOME>(l, go) : go(l);
+    if (e == cudaSuccess) return GC_OK;
+    cudaGetLastError();
+    return GC_ERR_CUDA;
 }
 
 unsigned grid_for(uint32_t tiles, int per_sm) {
@@ -488,11 +484,10 @@ int check_ws(const void* ws, size_t ws_bytes, int64_t n) {
     return !ws || ((uintptr_t)ws & 255) || ws_bytes < gc_grad_workspace_bytes(n) ? GC_ERR_WORKSPACE : GC_OK;
 }
 
-// The partial sums of the list; *slots how many.
-int launch_squares(const gc_tensor* list, int64_t n, double* part, int* slots, cudaStream_t st) {
-    *slots = 0;
-    return each_group(list, n, false, [&](const auto& l) {
-        if (l.tiles == 0) return cudaSuccess;
+// The partial sums of a group; *slots how many there are so far.
+int launch_squares(const List<MANY>& group, double* part, int* slots, cudaStream_t st) {
+    if (group.tiles == 0) return GC_OK;
+    return with_list(group, [&](const auto& l) {
         const unsigned grid = grid_for(l.tiles, GR_B1);
         using L = std::decay_t<decltype(l)>;
         const cudaError_t e = launch_chained(grad_square_kernel<sizeof(L::e) / sizeof(Entry)>, dim3(grid), GR_THREADS, 0,
@@ -501,17 +496,25 @@ int launch_squares(const gc_tensor* list, int64_t n, double* part, int* slots, c
         return e;
     });
 }
-int launch_scale(const gc_tensor* list, int64_t n, const double* part, int slots, float max_norm, double* sq_sum,
-                 float* norm, int* dev_status, cudaStream_t st) {
-    int tell = 1;
-    return each_group(list, n, true, [&](const auto& l) {
+int launch_scale(const List<MANY>& group, const double* part, int slots, float max_norm, double* sq_sum, float* norm,
+                 int* dev_status, bool tell, cudaStream_t st) {
+    return with_list(group, [&](const auto& l) {
         using L = std::decay_t<decltype(l)>;
-        const cudaError_t e =
-            launch_chained(grad_scale_kernel<sizeof(L::e) / sizeof(Entry)>, dim3(grid_for(l.tiles, GR_B2)), GR_THREADS, 0, 1, st,
-                           l, part, slots, max_norm, sq_sum, norm, dev_status, tell);
-        tell = 0;
-        return e;
+        return launch_chained(grad_scale_kernel<sizeof(L::e) / sizeof(Entry)>, dim3(grid_for(l.tiles, GR_B2)),
+                              GR_THREADS, 0, 1, st, l, part, slots, max_norm, sq_sum, norm, dev_status, tell ? 1 : 0);
     });
+}
+int scale_all(const gc_tensor* list, int64_t n, const double* part, int slots, float max_norm, double* sq_sum,
+              float* norm, int* dev_status, cudaStream_t st) {
+    List<MANY> group;
+    int64_t i = 0;
+    bool tell = true;
+    do {
+        int rc = next_group(list, n, true, &i, group);
+        if (rc || (rc = launch_scale(group, part, slots, max_norm, sq_sum, norm, dev_status, tell, st))) return rc;
+        tell = false;
+    } while (i < n);
+    return GC_OK;
 }
 
 }  // namespace
@@ -533,8 +536,12 @@ int gc_grad_norm(const gc_tensor* list, int64_t n, double* sq_sum, float* norm, 
     if (rc || (rc = check_ws(ws, ws_bytes, n)) || (rc = current_device())) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     double* part = static_cast<double*>(ws);
-    int slots;
-    if ((rc = launch_squares(list, n, part, &slots, st))) return rc;
+    List<MANY> group;
+    int64_t i = 0;
+    int slots = 0;
+    do {
+        if ((rc = next_group(list, n, false, &i, group)) || (rc = launch_squares(group, part, &slots, st))) return rc;
+    } while (i < n);
     if (launch_chained(grad_norm_kernel, dim3(1), GR_THREADS, 0, 1, st, part, slots, sq_sum, norm, dev_status) !=
         cudaSuccess) {
         cudaGetLastError();
@@ -551,8 +558,8 @@ int gc_grad_scale(const gc_tensor* list, int64_t n, const double* sq_sum, float 
     if (!(max_norm >= 0.f)) return GC_ERR_SHAPE;
     int rc = check_list(list, n, true);
     if (rc || (rc = current_device())) return rc;
-    return launch_scale(list, n, sq_sum, 1, max_norm, nullptr, nullptr, dev_status,
-                        static_cast<cudaStream_t>(cuda_stream));
+    return scale_all(list, n, sq_sum, 1, max_norm, nullptr, nullptr, dev_status,
+                     static_cast<cudaStream_t>(cuda_stream));
 } catch (...) {
     return GC_ERR_HOST;
 }
@@ -565,9 +572,15 @@ int gc_grad_clip(const gc_tensor* list, int64_t n, float max_norm, double* sq_su
     if (rc || (rc = check_ws(ws, ws_bytes, n)) || (rc = current_device())) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     double* part = static_cast<double*>(ws);
-    int slots;
-    if ((rc = launch_squares(list, n, part, &slots, st))) return rc;
-    return launch_scale(list, n, part, slots, max_norm, sq_sum, norm, dev_status, st);
+    List<MANY> group;
+    int64_t i = 0;
+    int slots = 0;
+    if ((rc = next_group(list, n, true, &i, group)) || (rc = launch_squares(group, part, &slots, st))) return rc;
+    if (i >= n)                                        // the only group: its list serves both passes
+        return launch_scale(group, part, slots, max_norm, sq_sum, norm, dev_status, true, st);
+    while (i < n)
+        if ((rc = next_group(list, n, true, &i, group)) || (rc = launch_squares(group, part, &slots, st))) return rc;
+    return scale_all(list, n, part, slots, max_norm, sq_sum, norm, dev_status, st);
 } catch (...) {
     return GC_ERR_HOST;
 }
