@@ -493,69 +493,71 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
             if (!mbar_wait(smem_u32(&bars.acc_full[use & 1]), (uint32_t)(use >> 1) & 1u, abort_flag)) break;
             tc_fence_after();
             const uint32_t src = tmem + (use & 1) * 256 + ((uint32_t)(32 * q) << 16);
-            if (row0 < p.rows_m) {
-                if (STAGED) {
-                    const int c0 = group * 64;
-#pragma unroll 1
-                    for (int y = 0; y < 2 && c0 < n; ++y) {                  // 32 columns each
-                        const int c = c0 + 32 * y;
-                        uint32_t v[32];
-                        tmem_ld32(src + c, v);
-                        if (y == 0) {
-                            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                            __syncwarp();
-                        }
-                        tmem_ld_wait();
-                        float f[32];
-                        scale_sums<32, true>(v, scales + 128 * y, mine, f);
-                        if (j0 + c + 32 > p.whole && p.whole < p.rows_n && i < p.rows_m) {
-                            // the columns after the last whole 16 bytes
+            // All of the warp's columns are read at once, so that the accumulator is free before anything is stored:
+            // the products of the tile after next start under this one's stores.
+            uint32_t v[2][32];
+            if (block != 16) {
+                tmem_ld32(src + (STAGED ? group * 64 : group * 32), v[0]);
+                tmem_ld32(src + (STAGED ? group * 64 + 32 : group * 32 + 128), v[1]);
+            } else {
+                uint32_t w[16];
+                tmem_ld16(src + group * 16, w);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const int64_t j = j0 + c + e;
-                                if (j >= p.whole && j < p.rows_n)
-                                    static_cast<__nv_bfloat16*>(p.out)[i * p.ldo + j] = __float2bfloat16_rn(f[e]);
-                            }
-                        }
-                        // 16-byte chunk k of row r lies at chunk k ^ (r & 7): the map's 128-byte swizzle
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                const __nv_bfloat162 h = __floats2bfloat162_rn(f[8 * k + 2 * z], f[8 * k + 2 * z + 1]);
-                                w[z] = *reinterpret_cast<const uint32_t*>(&h);
-                            }
-                            const uint32_t at = buf + lane * 128 + (((4 * y + k) ^ (lane & 7)) << 4);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                         ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                        }
-                        if (y == 1) {
-                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                            __syncwarp();
-                            if (lane == 0 && j0 + c0 < p.whole) tma_store_2d(&mapO, buf, (int)(j0 + c0), (int)row0);
-                        }
-                    }
-                } else if (block == 32) {
-#pragma unroll 1
-                    for (int y = 0; y < 2; ++y) {
-                        const int c = (4 * y + group) * 32;
-                        if (c >= n) break;
-                        uint32_t v[32];
-                        tmem_ld32(src + c, v);
-                        tmem_ld_wait();
-                        store_block<32, BF16>(v, scales + 128 * y, mine, p, j0 + c, n - c, i, lane);
-                    }
-                } else if (group * 16 < n) {
-                    uint32_t v[16];
-                    tmem_ld16(src + group * 16, v);
-                    tmem_ld_wait();
-                    store_block<16, BF16>(v, scales, mine, p, j0 + group * 16, n - group * 16, i, lane);
-                }
+                for (int e = 0; e < 16; ++e) v[0][e] = w[e];
             }
+            tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars.acc_free[use & 1]));
+            if (row0 >= p.rows_m) continue;
+            if (STAGED) {
+                const int c0 = group * 64;
+                if (c0 >= n) continue;
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                __syncwarp();
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {                                // 32 columns each
+                    const int c = c0 + 32 * y;
+                    float f[32];
+                    scale_sums<32, true>(v[y], scales + 128 * y, mine, f);
+                    if (j0 + c + 32 > p.whole && p.whole < p.rows_n && i < p.rows_m) {
+                        // the columns after the last whole 16 bytes
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int64_t j = j0 + c + e;
+                            if (j >= p.whole && j < p.rows_n)
+                                static_cast<__nv_bfloat16*>(p.out)[i * p.ldo + j] = __float2bfloat16_rn(f[e]);
+                        }
+                    }
+                    // 16-byte chunk k of row r lies at chunk k ^ (r & 7): the map's 128-byte swizzle
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(f[8 * k + 2 * z], f[8 * k + 2 * z + 1]);
+                            w[z] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
+                        const uint32_t at = buf + lane * 128 + (((4 * y + k) ^ (lane & 7)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                     ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0 && j0 + c0 < p.whole) tma_store_2d(&mapO, buf, (int)(j0 + c0), (int)row0);
+            } else if (block == 32) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int c = (4 * y + group) * 32;
+                    if (c < n) store_block<32, BF16>(v[y], scales + 128 * y, mine, p, j0 + c, n - c, i, lane);
+                }
+            } else if (group * 16 < n) {
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = v[0][e];
+                store_block<16, BF16>(w, scales, mine, p, j0 + group * 16, n - group * 16, i, lane);
+            }
         }
         if (STAGED) {
             if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
