@@ -26,6 +26,11 @@ constexpr int GR_PER = 4;                      // of a thread, all under way at 
 // 180 / 89 / 334, 3 and 2 177 / 88 / 332, 4 and 3 180 / 89 / 336; tiles of 16 KB 188 / 95 / 370, of 64 KB 179 / 90 / 332.
 constexpr int GR_B1 = 3, GR_B2 = 2;
 constexpr int GR_TILE_UNITS = GR_THREADS * GR_PER;   // 16-byte vectors of a tile; single elements where they do not fit
+constexpr int GR_CLUSTER = 16;
+// Lists of at most so many tiles take one launch of a cluster instead of two of the whole device.  Measured, us a call back to
+// back from the host, then in a graph, 8 tiles: norm 5.0 and 3.4 (two launches 7.0 and 3.2), clipping 5.3 and 5.4 (7.0
+// and 4.6); 16 tiles: clipping 5.5 and 5.5 (7.1 and 4.8); 36: 7.8 and 7.7 (7.1 and 4.9).
+constexpr uint32_t GR_SHORT = 16;
 constexpr int GR_SLOTS = 1024;                 // partial sums of a launch
 constexpr double GR_EPS = 1e-6;
 
@@ -157,6 +162,96 @@ __device__ __forceinline__ double block_sum(double v, double* part) {
     return s;
 }
 
+// A thread's share of the sum of squares of tile t of entry e (tid: of GR_THREADS).
+__device__ __forceinline__ double squares_of(const Entry& e, uint32_t t, int tid) {
+    const bool bf16 = e.bf16;
+    uint4 v[GR_PER];
+    if (e.mode == FLAT_VEC) {
+        const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + tid;
+        const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4) + 16 * u;
+        if (u - tid + GR_TILE_UNITS <= e.units) {
+#pragma unroll
+            for (int i = 0; i < GR_PER; ++i) v[i] = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < GR_PER; ++i)
+                v[i] = u + i * GR_THREADS < e.units ? *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i)
+                                                    : make_uint4(0, 0, 0, 0);
+        }
+        double sum = square_sum(v, bf16);
+        if (t == e.first && tid < e.head + e.tail) {
+            const double x = load_one(e.src, tid < e.head ? tid : tid + e.units * (bf16 ? 8 : 4), bf16);
+            sum = fma(x, x, sum);
+        }
+        return sum;
+    }
+    const Tile x = tile_of(e, t);
+    if (e.mode == ROWS_VEC) {
+#pragma unroll
+        for (int i = 0; i < GR_PER; ++i) {
+            const uint32_t k = tid + i * GR_THREADS;
+            v[i] = k < x.n ? *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
+                                                             place_of(e, x, k, e.ld) * (bf16 ? 2 : 4))
+                           : make_uint4(0, 0, 0, 0);
+        }
+        return square_sum(v, bf16);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < GR_PER; ++i) {
+        const uint32_t k = tid + i * GR_THREADS;
+        if (k < x.n) {
+            const double y = load_one(e.src, place_of(e, x, k, e.ld), bf16);
+            sum = fma(y, y, sum);
+        }
+    }
+    return sum;
+}
+// out = c g (copy: out = g) for a thread's share of tile t of entry e.
+__device__ __forceinline__ void scale_tile(const Entry& e, uint32_t t, int tid, bool copy, float c) {
+    const bool bf16 = e.bf16;
+    if (copy && e.src == e.dst) return;                  // the values stay as they are
+    if (e.mode == FLAT_VEC) {
+        const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + tid;
+        const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4) + 16 * u;
+        char* dst = static_cast<char*>(e.dst) + e.head * (bf16 ? 2 : 4) + 16 * u;
+        if (u - tid + GR_TILE_UNITS <= e.units) {
+            uint4 v[GR_PER];
+#pragma unroll
+            for (int i = 0; i < GR_PER; ++i) v[i] = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
+#pragma unroll
+            for (int i = 0; i < GR_PER; ++i)
+                *reinterpret_cast<uint4*>(dst + 16 * GR_THREADS * i) = copy ? v[i] : scale_vec(v[i], bf16, c);
+        } else {
+#pragma unroll
+            for (int i = 0; i < GR_PER; ++i)
+                if (u + i * GR_THREADS < e.units) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
+                    *reinterpret_cast<uint4*>(dst + 16 * GR_THREADS * i) = copy ? v : scale_vec(v, bf16, c);
+                }
+        }
+        if (t == e.first && tid < e.head + e.tail) {
+            const int64_t i = tid < e.head ? tid : tid + e.units * (bf16 ? 8 : 4);
+            scale_one(e, i, i, copy, c);
+        }
+        return;
+    }
+    const Tile x = tile_of(e, t);
+#pragma unroll
+    for (int i = 0; i < GR_PER; ++i) {
+        const uint32_t k = tid + i * GR_THREADS;
+        if (k >= x.n) break;
+        const int64_t from = place_of(e, x, k, e.ld), to = place_of(e, x, k, e.ld_out);
+        if (e.mode == ROWS_VEC) {
+            const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) + from * (bf16 ? 2 : 4));
+            *reinterpret_cast<uint4*>(static_cast<char*>(e.dst) + to * (bf16 ? 2 : 4)) =
+                copy ? v : scale_vec(v, bf16, c);
+        } else {
+            scale_one(e, from, to, copy, c);
+        }
+    }
+}
+
 // part[block] = the sum of squares of the block's tiles.
 template <int N>
 __global__ void __launch_bounds__(GR_THREADS, GR_B1)
@@ -168,49 +263,7 @@ grad_square_kernel(const __grid_constant__ List<N> list, double* part) {
     int at = 0;
     for (uint32_t t = blockIdx.x; t < list.tiles; t += gridDim.x) {
         at = entry_of(list, t, at, list.n - 1);
-        const Entry& e = list.e[at];
-        const bool bf16 = e.bf16;
-        uint4 v[GR_PER];
-        if (e.mode == FLAT_VEC) {
-            const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
-            const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4) + 16 * u;
-            if (u - threadIdx.x + GR_TILE_UNITS <= e.units) {
-#pragma unroll
-                for (int i = 0; i < GR_PER; ++i) v[i] = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
-            } else {
-#pragma unroll
-                for (int i = 0; i < GR_PER; ++i)
-                    v[i] = u + i * GR_THREADS < e.units ? *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i)
-                                                        : make_uint4(0, 0, 0, 0);
-            }
-            sum += square_sum(v, bf16);
-            if (t == e.first && threadIdx.x < e.head + e.tail) {
-                const int k = threadIdx.x;
-                const double x = load_one(e.src, k < e.head ? k : k + e.units * (bf16 ? 8 : 4), bf16);
-                sum = fma(x, x, sum);
-            }
-            continue;
-        }
-        const Tile x = tile_of(e, t);
-        if (e.mode == ROWS_VEC) {
-#pragma unroll
-            for (int i = 0; i < GR_PER; ++i) {
-                const uint32_t k = threadIdx.x + i * GR_THREADS;
-                v[i] = k < x.n ? *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) +
-                                                                 place_of(e, x, k, e.ld) * (bf16 ? 2 : 4))
-                               : make_uint4(0, 0, 0, 0);
-            }
-            sum += square_sum(v, bf16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < GR_PER; ++i) {
-                const uint32_t k = threadIdx.x + i * GR_THREADS;
-                if (k < x.n) {
-                    const double y = load_one(e.src, place_of(e, x, k, e.ld), bf16);
-                    sum = fma(y, y, sum);
-                }
-            }
-        }
+        sum += squares_of(list.e[at], t, threadIdx.x);
     }
     sum = block_sum(sum, warp_part);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -226,6 +279,14 @@ __device__ __forceinline__ void tell_norm(double total, double* sq_sum, float* n
     if (sq_sum) *sq_sum = total;
     if (norm) *norm = (float)sqrt(total);
     if (dev_status && !isfinite(total)) atomicOr(dev_status, GC_DEV_GRAD_NONFINITE);
+}
+
+// The factor of the gradients.  *copy: it is 1 or more, or the sum not finite, and values are copied bit for bit, a NaN's
+// payload too (told from the fp64 factor: by c == 1 the compiler takes a product with c for the same).
+__device__ __forceinline__ float factor_of(double total, float max_norm, bool* copy) {
+    const double wide = (double)max_norm / (sqrt(total) + GR_EPS);
+    *copy = !isfinite(total) || wide >= 1.0;
+    return (float)wide;
 }
 
 __global__ void __launch_bounds__(GR_THREADS)
@@ -247,59 +308,52 @@ grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int 
     dep_wait();
     const double total = total_of(part, slots, warp_part);
     if (tell && blockIdx.x == 0 && threadIdx.x == 0) tell_norm(total, sq_sum, norm, dev_status);
-    // c >= 1, or a sum that is not finite: values are copied bit for bit, a NaN's payload too (told from the fp64
-    // factor: by c == 1 the compiler takes a product with c for the same)
-    const double wide = (double)max_norm / (sqrt(total) + GR_EPS);
-    const bool copy = !isfinite(total) || wide >= 1.0;
-    const float c = (float)wide;
+    bool copy;
+    const float c = factor_of(total, max_norm, &copy);
     // backwards: what the sum of squares read last is in the L2 still
     int at = list.n - 1;
     for (int64_t back = (int64_t)list.tiles - 1 - blockIdx.x; back >= 0; back -= gridDim.x) {
         const uint32_t t = (uint32_t)back;
         at = entry_of(list, t, 0, at);
-        const Entry& e = list.e[at];
-        const bool bf16 = e.bf16;
-        if (copy && e.src == e.dst) continue;            // the values stay as they are
-        if (e.mode == FLAT_VEC) {
-            const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + threadIdx.x;
-            const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4) + 16 * u;
-            char* dst = static_cast<char*>(e.dst) + e.head * (bf16 ? 2 : 4) + 16 * u;
-            if (u - threadIdx.x + GR_TILE_UNITS <= e.units) {
-                uint4 v[GR_PER];
-#pragma unroll
-                for (int i = 0; i < GR_PER; ++i) v[i] = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
-#pragma unroll
-                for (int i = 0; i < GR_PER; ++i)
-                    *reinterpret_cast<uint4*>(dst + 16 * GR_THREADS * i) = copy ? v[i] : scale_vec(v[i], bf16, c);
-            } else {
-#pragma unroll
-                for (int i = 0; i < GR_PER; ++i)
-                    if (u + i * GR_THREADS < e.units) {
-                        const uint4 v = *reinterpret_cast<const uint4*>(src + 16 * GR_THREADS * i);
-                        *reinterpret_cast<uint4*>(dst + 16 * GR_THREADS * i) = copy ? v : scale_vec(v, bf16, c);
-                    }
-            }
-            if (t == e.first && threadIdx.x < e.head + e.tail) {
-                const int k = threadIdx.x;
-                const int64_t i = k < e.head ? k : k + e.units * (bf16 ? 8 : 4);
-                scale_one(e, i, i, copy, c);
-            }
-            continue;
-        }
-        const Tile x = tile_of(e, t);
-#pragma unroll
-        for (int i = 0; i < GR_PER; ++i) {
-            const uint32_t k = threadIdx.x + i * GR_THREADS;
-            if (k >= x.n) break;
-            const int64_t from = place_of(e, x, k, e.ld), to = place_of(e, x, k, e.ld_out);
-            if (e.mode == ROWS_VEC) {
-                const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(e.src) + from * (bf16 ? 2 : 4));
-                *reinterpret_cast<uint4*>(static_cast<char*>(e.dst) + to * (bf16 ? 2 : 4)) =
-                    copy ? v : scale_vec(v, bf16, c);
-            } else {
-                scale_one(e, from, to, copy, c);
-            }
-        }
+        scale_tile(list.e[at], t, threadIdx.x, copy, c);
+    }
+}
+
+// Short lists: both passes in one cluster, whose CTAs exchange their sums through shared memory.  Two halves of a CTA
+// take a tile each.
+template <int N, bool CLIP>
+__global__ void __launch_bounds__(2 * GR_THREADS, 1)
+grad_cluster_kernel(const __grid_constant__ List<N> list, float max_norm, double* sq_sum, float* norm, int* dev_status) {
+    __shared__ double warp_part[2 * GR_THREADS / 32];
+    __shared__ double sums[GR_CLUSTER];
+    const int tid = threadIdx.x % GR_THREADS, ctas = gridDim.x;
+    const uint32_t first = 2 * blockIdx.x + threadIdx.x / GR_THREADS, by = 2 * ctas;
+    dep_release();
+    dep_wait();
+    double sum = 0.0;
+    int at = 0;
+    for (uint32_t t = first; t < list.tiles; t += by) {
+        at = entry_of(list, t, at, list.n - 1);
+        sum += squares_of(list.e[at], t, tid);
+    }
+    sum = block_sum(sum, warp_part);
+    if ((int)threadIdx.x < ctas) {
+        uint32_t there;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                     : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x])), "r"(threadIdx.x));
+        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(there), "d"(sum) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
+                 "barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    double total = 0.0;
+    for (int i = 0; i < ctas; ++i) total += sums[i];
+    if (blockIdx.x == 0 && threadIdx.x == 0) tell_norm(total, sq_sum, norm, dev_status);
+    if (!CLIP) return;
+    bool copy;
+    const float c = factor_of(total, max_norm, &copy);
+    for (uint32_t t = first; t < list.tiles; t += by) {
+        at = entry_of(list, t, 0, list.n - 1);
+        scale_tile(list.e[at], t, tid, copy, c);
     }
 }
 
@@ -504,6 +558,34 @@ int launch_scale(const List<MANY>& group, const double* part, int slots, float m
                               GR_THREADS, 0, 1, st, l, part, slots, max_norm, sq_sum, norm, dev_status, tell ? 1 : 0);
     });
 }
+// Lists short enough for one cluster.
+bool is_short(const List<MANY>& group) { return group.tiles <= GR_SHORT && group.n <= FEW; }
+template <bool CLIP>
+int launch_short(const List<MANY>& group, float max_norm, double* sq_sum, float* norm, int* dev_status, cudaStream_t st) {
+    int dev = 0;
+    static bool configured_on[64] = {false};             // the attribute belongs to (kernel, device)
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return GC_ERR_CUDA;
+    }
+    if (!configured_on[dev]) {
+        if (cudaFuncSetAttribute(grad_cluster_kernel<FEW, CLIP>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+            cudaSuccess) {
+            cudaGetLastError();
+            return GC_ERR_CUDA;
+        }
+        configured_on[dev] = true;
+    }
+    int ctas = 1;
+    while (ctas < GR_CLUSTER && 2u * ctas < group.tiles) ctas *= 2;
+    const cudaError_t e = with_size<FEW>(group, [&](const List<FEW>& l) {
+        return launch_chained(grad_cluster_kernel<FEW, CLIP>, dim3(ctas), 2 * GR_THREADS, 0, ctas, st, l, max_norm, sq_sum,
+                              norm, dev_status);
+    });
+    if (e == cudaSuccess) return GC_OK;
+    cudaGetLastError();
+    return GC_ERR_CUDA;
+}
 int scale_all(const gc_tensor* list, int64_t n, const double* part, int slots, float max_norm, double* sq_sum,
               float* norm, int* dev_status, cudaStream_t st) {
     List<MANY> group;
@@ -539,9 +621,11 @@ int gc_grad_norm(const gc_tensor* list, int64_t n, double* sq_sum, float* norm, 
     List<MANY> group;
     int64_t i = 0;
     int slots = 0;
-    do {
+    if ((rc = next_group(list, n, false, &i, group))) return rc;
+    if (i >= n && is_short(group)) return launch_short<false>(group, 0.f, sq_sum, norm, dev_status, st);
+    if ((rc = launch_squares(group, part, &slots, st))) return rc;
+    while (i < n)
         if ((rc = next_group(list, n, false, &i, group)) || (rc = launch_squares(group, part, &slots, st))) return rc;
-    } while (i < n);
     if (launch_chained(grad_norm_kernel, dim3(1), GR_THREADS, 0, 1, st, part, slots, sq_sum, norm, dev_status) !=
         cudaSuccess) {
         cudaGetLastError();
@@ -575,7 +659,9 @@ int gc_grad_clip(const gc_tensor* list, int64_t n, float max_norm, double* sq_su
     List<MANY> group;
     int64_t i = 0;
     int slots = 0;
-    if ((rc = next_group(list, n, true, &i, group)) || (rc = launch_squares(group, part, &slots, st))) return rc;
+    if ((rc = next_group(list, n, true, &i, group))) return rc;
+    if (i >= n && is_short(group)) return launch_short<true>(group, max_norm, sq_sum, norm, dev_status, st);
+    if ((rc = launch_squares(group, part, &slots, st))) return rc;
     if (i >= n)                                        // the only group: its list serves both passes
         return launch_scale(group, part, slots, max_norm, sq_sum, norm, dev_status, true, st);
     while (i < n)

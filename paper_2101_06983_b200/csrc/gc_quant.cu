@@ -637,7 +637,7 @@ struct ImPlan { bool pair, staged; int bn; };
 
 // The tile that costs least by a count of cycles: rounds of tiles, each its products or loads, whichever is longer, or
 // its stores where they are longer still, and the stores of the last one.  The constants are fitted to 72 shapes with every
-// choice forced, one row to 60000 and contractions of 40 to 8192: 2 % behind the best choice on average, 14 % at
+// choice forced, one row to 60000 and contractions of 40 to 8192: 2.5 % behind the best choice on average, 20 % at
 // most.  bf16 outputs without staging would be 7 % behind (69 % at most), all of them staged 6 (60).
 ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, bool bf16) {
     ImPlan best{false, false, 16};
