@@ -343,10 +343,10 @@ int gc_dist_dot_block(const void* Q, int64_t ldq, const void* P, int64_t ldp, in
  * Squares are summed in fp32 over at most 64 values and in fp64 beyond, and in fp64 throughout where they
  * overflow or vanish in fp32: n is off by at most 2^-20 n for any finite values.  c is rounded to fp32,
  * then c g to the tensor's type.  Where n^2 is not finite (a NaN or an infinity among the gradients) *dev_status (may be NULL) gets
- * GC_DEV_GRAD_NONFINITE and c is 1: the values stay as they are, or are copied as they are.
+ * GC_DEV_GRAD_NONFINITE and c is 1 (so it is for a *sq_sum that is negative): the values stay as they are, or are copied as they are.
  * max_norm >= 0 (an infinity never scales); NaN or negative: GC_ERR_SHAPE.
- * Workspace: gc_grad_workspace_bytes(n_tensors), 256-byte aligned, 0 for invalid arguments.  Asynchronous on
- * cuda_stream, deterministic.
+ * Workspace: gc_grad_workspace_bytes(n_tensors), 256-byte aligned, 0 for invalid arguments; calls that may
+ * overlap on the GPU need one each.  Asynchronous on cuda_stream, deterministic.
  */
 typedef struct {
     void* data;            /* [rows x cols], row pitch ld (elements; not read for one row) */
@@ -379,9 +379,9 @@ int gc_grad_clip(const gc_tensor* tensors, int64_t n_tensors, float max_norm, do
  *                      inputs and B the quantised W, out is the encoder's output; with A and B quantised
  *                      representations, out is S times tau.
  * X [rows x d] of dtype (GC_F32 or GC_BF16); q, A, B int8; scales float; leading dimensions in elements, every
- * row of X, q, A, B and out starts on a 16-byte boundary (else GC_ERR_ALIGN; widths need no padding, and what lies
- * between a row's end and the next row is neither read as a value nor written).  Any widths; at most 2^30
- * rows.  A and B may be the same buffer.  Asynchronous on cuda_stream, deterministic; no workspace.
+ * row of X, q, A, B and out starts on a 16-byte boundary (else GC_ERR_ALIGN; widths need no padding, what lies
+ * between a row's end and the next row is neither read as a value nor written, and a single row's leading dimension
+ * is not read).  At most 2^30 rows and columns (else GC_ERR_LIMIT).  A and B may be the same buffer.  Asynchronous on cuda_stream, deterministic; no workspace.
  * GC_DEV_WAIT_LIMIT in *dev_status (may be NULL) as for the other calls.
  */
 int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dtype, int8_t* q, int64_t ldq,

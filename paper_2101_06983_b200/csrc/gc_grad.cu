@@ -278,14 +278,14 @@ __device__ __forceinline__ double total_of(const double* part, int slots, double
 __device__ __forceinline__ void tell_norm(double total, double* sq_sum, float* norm, int* dev_status) {
     if (sq_sum) *sq_sum = total;
     if (norm) *norm = (float)sqrt(total);
-    if (dev_status && !isfinite(total)) atomicOr(dev_status, GC_DEV_GRAD_NONFINITE);
+    if (dev_status && !isfinite(sqrt(total))) atomicOr(dev_status, GC_DEV_GRAD_NONFINITE);
 }
 
 // The factor of the gradients.  *copy: it is 1 or more, or the sum not finite, and values are copied bit for bit, a NaN's
 // payload too (told from the fp64 factor: by c == 1 the compiler takes a product with c for the same).
 __device__ __forceinline__ float factor_of(double total, float max_norm, bool* copy) {
-    const double wide = (double)max_norm / (sqrt(total) + GR_EPS);
-    *copy = !isfinite(total) || wide >= 1.0;
+    const double norm = sqrt(total), wide = (double)max_norm / (norm + GR_EPS);
+    *copy = !isfinite(norm) || wide >= 1.0;
     return (float)wide;
 }
 

@@ -263,6 +263,11 @@ __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint32_t a_lo, uint32_t 
     }
 }
 
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 // The products of 32 lanes' sums with the scales of the N side's rows (in shared memory) and of the lane's row; the
 // order is a_scale first.
 template <int G, bool LANE_FIRST>
@@ -485,6 +490,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
             const int64_t j0 = (int64_t)tn * p.bn;
             const int n = (int)min((int64_t)p.bn, p.rows_n - j0);
             const float mine = next_m;
+            __syncwarp();                          // every lane has read the last tile's
 #pragma unroll
             for (int x = 0; x < 2; ++x)
                 asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + 4 * (32 * x + lane)), "f"(next_n[x]) : "memory");
@@ -601,11 +607,14 @@ bool make_map_i8(CUtensorMap* map, const void* base, int64_t rows, int64_t k, in
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int check_matrix(const void* base, int64_t rows, int64_t cols, int64_t ld, int es) {
+// Checks a matrix; a single row has no pitch, *ld becomes one that the checks of several rows would pass.
+int check_matrix(const void* base, int64_t rows, int64_t cols, int64_t* ld, int es) {
     if (!base) return GC_ERR_NULL;
-    if (rows <= 0 || cols <= 0 || ld < cols || ld > ((int64_t)1 << 36)) return GC_ERR_SHAPE;
+    if (rows <= 0 || cols <= 0) return GC_ERR_SHAPE;
     if (rows > ((int64_t)1 << 30) || cols > ((int64_t)1 << 30)) return GC_ERR_LIMIT;
-    if (((uintptr_t)base & 15) || (ld * es) % 16 != 0) return GC_ERR_ALIGN;
+    if (rows == 1) *ld = (cols + 15) & ~(int64_t)15;
+    if (*ld < cols || *ld > ((int64_t)1 << 36)) return GC_ERR_SHAPE;
+    if (((uintptr_t)base & 15) || (*ld * es) % 16 != 0) return GC_ERR_ALIGN;
     return GC_OK;
 }
 int check_device(int* dev) {
@@ -681,8 +690,8 @@ extern "C" {
 int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dtype, int8_t* q, int64_t ldq,
                      float* scale, void* cuda_stream) {
     if (dtype != GC_F32 && dtype != GC_BF16) return GC_ERR_DTYPE;
-    int rc = check_matrix(X, rows, d, ldx, dtype == GC_BF16 ? 2 : 4);
-    if (rc || (rc = check_matrix(q, rows, d, ldq, 1))) return rc;
+    int rc = check_matrix(X, rows, d, &ldx, dtype == GC_BF16 ? 2 : 4);
+    if (rc || (rc = check_matrix(q, rows, d, &ldq, 1))) return rc;
     if (!scale) return GC_ERR_NULL;
     int dev;
     if ((rc = check_device(&dev))) return rc;
@@ -717,9 +726,9 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
                  const float* b_scale, int64_t rows, int64_t cols, int64_t k, int out_dtype, void* out, int64_t ldo,
                  int* dev_status, void* cuda_stream) {
     if (out_dtype != GC_F32 && out_dtype != GC_BF16) return GC_ERR_DTYPE;
-    int rc = check_matrix(A, rows, k, lda, 1);
-    if (rc || (rc = check_matrix(B, cols, k, ldb, 1)) ||
-        (rc = check_matrix(out, rows, cols, ldo, out_dtype == GC_BF16 ? 2 : 4)))
+    int rc = check_matrix(A, rows, k, &lda, 1);
+    if (rc || (rc = check_matrix(B, cols, k, &ldb, 1)) ||
+        (rc = check_matrix(out, rows, cols, &ldo, out_dtype == GC_BF16 ? 2 : 4)))
         return rc;
     if (!a_scale || !b_scale) return GC_ERR_NULL;
     if (k > 131071) return GC_ERR_LIMIT;           // 2^14 (k of -128 times -128) must fit 31 bits

@@ -358,11 +358,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 
 // Instruction descriptor, kind::f16: fp32 accumulate, bf16 A and B, M = 128.
 __device__ __forceinline__ uint32_t instr_desc(int n, bool b_mn_major, int m = XROWS,

@@ -126,6 +126,14 @@ class LibraryKernels:
         binding.gc_shard_dp(Q_all, P_all, pos_all, tau, row_lse, p0, p_count, dP, ws=ws,
                             dev_status=status, mask_mode=mask_mode)
 
+    def grad_sq_sum(self, grads, sq_sum, ws, dev_status):
+        from . import binding
+        binding.gc_grad_norm(grads, sq_sum=sq_sum, ws=ws, dev_status=dev_status)
+
+    def grad_scale(self, grads, sq_sum, max_norm, dev_status):
+        from . import binding
+        binding.gc_grad_scale(grads, sq_sum, max_norm, dev_status=dev_status)
+
 
 class ShardedStep:
     """One sharded Step 2 for a fixed problem size, reusable across calls.
@@ -209,3 +217,18 @@ def sharded_build_cache(Q_local, P_local, pos_local, tau, B, N, kernels=None, gr
     step = ShardedStep(B, N, Q_local.shape[1], Q_local.dtype, Q_local.device, kernels, group,
                        mask_mode)
     return step.run(Q_local, P_local, pos_local, tau)
+
+
+def clip_over_ranks(grads, max_norm, sq_sum, ws=None, dev_status=None, kernels=None, group=None):
+    """Clips gradients of which every rank holds another part (after Step 3 and a reduce-scatter of dW, each rank
+    its slice) by their norm over all ranks: sums of squares, one all-reduce of a double, scaling.  Afterwards
+    sq_sum[0] (float64) is the square of that norm on every rank.  `grads`: a binding.GradList, made once for buffers
+    that stay, or tensors.  A value that is not finite on one rank leaves the gradients of all ranks as they are
+    and sets GC_DEV_GRAD_NONFINITE in everyone's dev_status.  Gradients that are the same on all ranks (an
+    all-reduce of dW) need no exchange: binding.gc_grad_clip."""
+    kernels = kernels or LibraryKernels()
+    kernels.grad_sq_sum(grads, sq_sum, ws, dev_status)
+    if _world(group)[0] > 1:
+        dist.all_reduce(sq_sum, op=dist.ReduceOp.SUM, group=group)
+    kernels.grad_scale(grads, sq_sum, max_norm, dev_status)
+    return sq_sum

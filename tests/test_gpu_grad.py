@@ -248,6 +248,18 @@ def test_values_that_are_not_finite(binding, dtype, bad):
         assert place.st.item() == binding.GC_DEV_GRAD_NONFINITE
 
 
+def test_sums_that_are_no_sums(binding):
+    """gc_grad_scale with a sum of squares that no gradients have: values stay, the flag is set."""
+    x = torch.randn(70000, device="cuda")
+    before = x.clone()
+    for bad in (-1.0, math.nan, math.inf):
+        sq = torch.tensor([bad], dtype=torch.float64, device="cuda")
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        binding.gc_grad_scale([x], sq, 1e-3, st)
+        torch.cuda.synchronize()
+        assert torch.equal(x, before) and st.item() == binding.GC_DEV_GRAD_NONFINITE
+
+
 def test_sums_of_two_ranks(binding):
     """Gradients that two ranks hold in part: each norms its own, the sums are added, each scales its own."""
     whole = torch.randn(70000, device="cuda")
@@ -263,6 +275,24 @@ def test_sums_of_two_ranks(binding):
     torch.cuda.synchronize()
     c = _factor(total.item(), 2.0)
     assert torch.equal(torch.cat(parts).cpu(), _scaled(whole, c))
+
+
+def test_clip_over_ranks_of_one(binding):
+    """The library's calls behind sharded.clip_over_ranks, with one rank."""
+    from paper_2101_06983_b200 import sharded
+    xs = [torch.randn(5000, device="cuda"), torch.randn(300, 7, device="cuda").to(BF)]
+    before = [x.clone() for x in xs]
+    sq = torch.zeros(1, dtype=torch.float64, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = sharded.clip_over_ranks(binding.GradList(xs), 1.5, sq, dev_status=st)
+    assert got is sq and abs(sq.item() - _sum64(before)) <= 2 * TOL_NORM * _sum64(before)
+    for x, b in zip(xs, before):
+        assert torch.equal(x.cpu(), _scaled(b, _factor(sq.item(), 1.5)))
+    xs[1][4, 2] = math.nan
+    before = [x.clone() for x in xs]
+    sharded.clip_over_ranks(xs, 0.1, sq, dev_status=st)
+    assert st.item() == binding.GC_DEV_GRAD_NONFINITE
+    assert torch.equal(xs[0], before[0]) and torch.equal(xs[1].view(torch.int16), before[1].view(torch.int16))
 
 
 def test_captured_calls_that_share_a_workspace(binding):

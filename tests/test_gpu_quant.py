@@ -188,6 +188,30 @@ def test_the_longest_contraction(binding, rows):
     assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("cols,k", [(1001, 77), (7, 768), (4097, 1)])
+def test_single_rows_need_no_pitch(binding, cols, k, dtype):
+    """One query of any width into contiguous tensors of those widths."""
+    x = torch.randn(1, k, device="cuda")
+    q, s = torch.empty(1, k, dtype=torch.int8, device="cuda"), torch.empty(1, device="cuda")
+    binding.gc_quantize_rows(x, q, s)
+    want_q, want_s = _quantized(x)
+    assert torch.equal(q.cpu(), want_q) and torch.equal(s.cpu(), want_s)
+    _, _, B, sb = _operands(1, cols, k, seed=cols)
+    guard = torch.full((cols + 16,), 5.0, dtype=dtype, device="cuda")
+    out = guard[:cols].view(1, cols)
+    binding.gc_matmul_i8(q, s, B, sb, out)
+    assert torch.equal(out, _product(q, s, B, sb, dtype)) and bool((guard[cols:] == 5).all())
+    # and one channel
+    out = torch.empty(cols, 1, dtype=dtype, device="cuda")
+    wide = torch.empty(cols, 8, dtype=dtype, device="cuda")[:, :1]
+    binding.gc_matmul_i8(B, sb, q, s, wide)
+    assert torch.equal(wide, _product(B, sb, q, s, dtype))
+    with pytest.raises(binding.GradCacheError) as e:
+        binding.gc_matmul_i8(B, sb, q, s, out)                  # rows of 2 or 4 bytes
+    assert e.value.status == 5
+
+
 def test_one_buffer_on_both_sides(binding):
     A, sa, _, _ = _operands(300, 1, 200, seed=1)
     _check_product(binding, A, sa, A, sa, F32)
