@@ -328,6 +328,7 @@ grad_cluster_kernel(const __grid_constant__ List<N> list, float max_norm, double
     __shared__ double sums[GR_CLUSTER];
     const int tid = threadIdx.x % GR_THREADS, ctas = gridDim.x;
     const uint32_t first = 2 * blockIdx.x + threadIdx.x / GR_THREADS, by = 2 * ctas;
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // this CTA has started
     dep_release();
     dep_wait();
     double sum = 0.0;
@@ -337,6 +338,7 @@ grad_cluster_kernel(const __grid_constant__ List<N> list, float max_norm, double
         sum += squares_of(list.e[at], t, tid);
     }
     sum = block_sum(sum, warp_part);
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");                // and so have those it sends to
     if ((int)threadIdx.x < ctas) {
         uint32_t there;
         asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"

@@ -9,10 +9,6 @@
 #include <math.h>
 
 #include <algorithm>
-#ifdef IM_TUNE
-#include <stdio.h>
-#include <stdlib.h>
-#endif
 
 #include "tc_common.cuh"
 
@@ -593,6 +589,153 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
     }
 }
 
+// Few rows of A and few tiles: a cluster of CTAs shares a tile of 128 rows of B x bn rows of A.  Each CTA takes a run of
+// the contraction blocks, and its sums of columns c .. go to the CTA that owns them (bn / ctas columns each),
+// through shared memory; sums of integers have no order.
+constexpr int SP_THREADS = 32 * (NPROD + 1 + 8);
+constexpr int SP_MAX_CTAS = 8;
+constexpr int SP_MAX_BN = 64;
+template <bool BF16>
+__global__ void __launch_bounds__(SP_THREADS, 1)
+matmul_i8_split_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant__ CUtensorMap mapN,
+                       const ImParams p, const int ctas) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) ImBars bars;
+    __shared__ uint32_t tmem_s;
+    __shared__ int abort_s;
+    volatile int* abort_flag = &abort_s;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
+    const int lane = threadIdx.x & 31;
+    const int rank = (int)cluster_ctarank();
+    const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t stage_bytes = CHUNK_BYTES + (uint32_t)p.bn * 128u;
+    const uint32_t sums = smem + p.stages * stage_bytes;           // [source CTA][own column][row of B]
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // this CTA has started
+    if (threadIdx.x == 0) {
+        abort_s = 0;
+        for (int s = 0; s < IM_MAX_ST; ++s) {
+            mbar_init(smem_u32(&bars.full[s]), 2);
+            mbar_init(smem_u32(&bars.empty[s]), 1);
+        }
+        mbar_init(smem_u32(&bars.acc_full[0]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(&tmem_s)), "r"((uint32_t)SP_MAX_BN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_s;
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");                // and so have those it will send to
+    dep_release();
+    dep_wait();
+
+    const int tm = (int)(blockIdx.x / (unsigned)ctas);
+    const int kb0 = (int)((int64_t)p.kblocks * rank / ctas), kb1 = (int)((int64_t)p.kblocks * (rank + 1) / ctas);
+    const int own = p.bn / ctas;                                   // columns of a CTA
+    const int64_t row = (int64_t)tm * 128;
+    if (warp < NPROD) {
+        const bool is_m = warp == 0;
+        const uint32_t bytes = is_m ? CHUNK_BYTES : (uint32_t)p.bn * 128u;
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int kb = kb0; kb < kb1 && ok; ++kb) {
+            ok = mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag);
+            if (!ok) break;
+            const uint32_t full = smem_u32(&bars.full[stage]);
+            if (elect_one()) {
+                mbar_expect_tx(full, bytes);
+                tma_load_2d(smem + stage * stage_bytes + (is_m ? 0u : CHUNK_BYTES), is_m ? &mapM : &mapN, kb * IM_KB,
+                            is_m ? (int)row : 0, full);
+            }
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+        for (int n = 0; n < p.stages && ok; ++n) {                 // every load and commit is done when the CTA leaves
+            ok = mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag);
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+    } else if (warp == MMA_WARP) {
+        const uint32_t idesc = instr_desc_i8(p.bn, 128);
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            if (!mbar_wait(smem_u32(&bars.full[stage]), phase, abort_flag)) break;
+            tc_fence_after();
+            const uint32_t m = desc_lo(smem + stage * stage_bytes, 0);
+            const uint32_t n = desc_lo(smem + stage * stage_bytes + CHUNK_BYTES, 0);
+            if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma_i8<false>(tmem, m + 2 * k, n + 2 * k, idesc, kb != kb0 || k != 0);
+                tc_commit(smem_u32(&bars.empty[stage]));
+                if (kb == kb1 - 1) tc_commit(smem_u32(&bars.acc_full[0]));
+            }
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+    } else {
+        // 32 rows of B, every other 16 columns
+        const int q = warp & 3, half = (warp - MMA_WARP - 1) >> 2;
+        if (mbar_wait(smem_u32(&bars.acc_full[0]), 0, abort_flag)) {
+            __syncwarp();
+            tc_fence_after();
+            for (int c = 16 * half; c < p.bn; c += 32) {
+                uint32_t v[16];
+                tmem_ld16(tmem + ((uint32_t)(32 * q) << 16) + c, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int to = (c + e) / own, col = (c + e) - to * own;
+                    asm volatile("st.shared::cluster.b32 [%0], %1;"
+                                 ::"r"(mapa_u32(sums + (uint32_t)(((rank * own + col) * 128 + 32 * q + lane) * 4), to)),
+                                   "r"(v[e]) : "memory");
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        // let bulk copies still in flight land before the shared memory is released
+        uint64_t t0 = global_ns();
+        while (global_ns() - t0 < 200000ull) __nanosleep(1000);
+        if (threadIdx.x == 0 && p.dev_status) atomicOr(p.dev_status, GC_DEV_WAIT_LIMIT);
+        __syncthreads();
+    }
+    cluster_sync_all();            // everyone's sums have arrived; nobody sends any more
+    if (warp == MMA_WARP) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;"
+                     ::"r"(tmem), "r"((uint32_t)SP_MAX_BN) : "memory");
+    }
+    if (warp > MMA_WARP) {
+        const int t = threadIdx.x - 32 * (MMA_WARP + 1), r = t & 127;
+        const int64_t j = row + r;
+        const float sb = j < p.rows_m ? p.m_scale[j] : 0.f;
+        for (int col = t >> 7; col < own; col += 2) {
+            const int64_t i = (int64_t)rank * own + col;
+            if (i >= p.rows_n || j >= p.rows_m) break;
+            const float sa = p.n_scale[i];
+            int v[SP_MAX_CTAS];
+#pragma unroll
+            for (int from = 0; from < SP_MAX_CTAS; ++from) {
+                v[from] = 0;
+                if (from < ctas)
+                    asm volatile("ld.shared.b32 %0, [%1];"
+                                 : "=r"(v[from]) : "r"(sums + (uint32_t)(((from * own + col) * 128 + r) * 4)));
+            }
+            int total = 0;
+#pragma unroll
+            for (int from = 0; from < SP_MAX_CTAS; ++from) total += v[from];
+            const float f = (float)total * sa * sb;
+            if (BF16) static_cast<__nv_bfloat16*>(p.out)[i * p.ldo + j] = __float2bfloat16_rn(f);
+            else      static_cast<float*>(p.out)[i * p.ldo + j] = f;
+        }
+    }
+}
+
 // ---- host ------------------------------------------------------------------------------------------
 // Row-major bytes [rows x k], boxes of box_rows x 128 bytes, 128-byte swizzle, zeros past the ends.
 bool make_map_i8(CUtensorMap* map, const void* base, int64_t rows, int64_t k, int64_t ld, int box_rows) {
@@ -651,13 +794,6 @@ struct ImPlan { bool pair, staged; int bn; };
 ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, bool bf16) {
     ImPlan best{false, false, 16};
     double least = INFINITY;
-#ifdef IM_TUNE
-    if (getenv("IM_PLAN")) {
-        int a, b, c;
-        sscanf(getenv("IM_PLAN"), "%d,%d,%d", &a, &b, &c);
-        return ImPlan{a != 0, b != 0, c};
-    }
-#endif
     const double kblocks = (double)((k + IM_KB - 1) / IM_KB);
     for (int staged = 0; staged < (bf16 && cols >= 8 ? 2 : 1); ++staged) {
         const int64_t m = staged ? rows : cols, n = staged ? cols : rows;
@@ -678,6 +814,47 @@ ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, bool bf16) {
             }
     }
     return best;
+}
+
+// CTAs to share a tile of few rows of A (1: none do).  The exchange costs as much as a few contraction blocks, more with
+// more rows.  Measured, us with 1 / 4 / 8 CTAs: 1 x 768 x 4096 6.5 / 4.8 / 4.1, 1 x 4096 x 4096 6.8 / 5.5 / -, 1 x 1024 x
+// 16384 18.6 / 9.4 / 6.3, 1 x 768 x 2048 4.8 / 4.2 / 3.8, 1 x 768 x 1024 3.6 / 3.8 / 3.6, 16 x 768 x 2048 4.6 / 4.1 / 3.7,
+// 64 x 768 x 2048 4.8 / 5.9 / 5.3, 64 x 768 x 4096 6.7 / 6.7 / 5.7, 64 x 4096 x 4096 7.0 / 7.2 / -; two never pay.
+int split_ctas(int64_t rows, int64_t cols, int64_t k) {
+    const int64_t tiles = (cols + 127) / 128, kblocks = (k + IM_KB - 1) / IM_KB;
+    if (rows > SP_MAX_BN || kblocks < (rows <= 16 ? 16 : 32)) return 1;
+    if (tiles * 8 <= sm_count()) return 8;
+    return rows <= 16 && tiles * 4 <= sm_count() ? 4 : 1;
+}
+int launch_split(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb, const float* b_scale,
+                 int64_t rows, int64_t cols, int64_t k, bool bf16, void* out, int64_t ldo, int ctas, int* dev_status,
+                 int dev, cudaStream_t st) {
+    ImParams p{};
+    p.rows_m = cols; p.rows_n = rows;
+    p.m_scale = b_scale; p.n_scale = a_scale;
+    p.kblocks = (int)((k + IM_KB - 1) / IM_KB);
+    p.bn = (int)((rows + 15) / 16 * 16);
+    p.tiles_m = (int)((cols + 127) / 128);
+    p.stages = std::min(IM_MAX_ST, (int)((IM_SMEM - 1024 - p.bn * 512) / (CHUNK_BYTES + (size_t)p.bn * 128)));
+    p.out = out; p.ldo = ldo; p.dev_status = dev_status;
+    CUtensorMap mm, mn;
+    if (!make_map_i8(&mm, B, cols, k, ldb, 128) || !make_map_i8(&mn, A, rows, k, lda, p.bn)) return GC_ERR_CUDA;
+    static bool configured_on[64] = {false};       // the attribute belongs to (kernel, device)
+    if (!configured_on[dev]) {
+        if (cudaFuncSetAttribute(matmul_i8_split_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)IM_SMEM) != cudaSuccess ||
+            cudaFuncSetAttribute(matmul_i8_split_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)IM_SMEM) != cudaSuccess) {
+            cudaGetLastError();
+            return GC_ERR_CUDA;
+        }
+        configured_on[dev] = true;
+    }
+    const cudaError_t e = launch_chained(bf16 ? matmul_i8_split_kernel<true> : matmul_i8_split_kernel<false>,
+                                         dim3((unsigned)p.tiles_m * ctas), SP_THREADS, IM_SMEM, ctas, st, mm, mn, p, ctas);
+    if (e == cudaSuccess) return GC_OK;
+    cudaGetLastError();
+    return GC_ERR_CUDA;
 }
 
 }  // namespace
@@ -735,6 +912,9 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     int dev;
     if ((rc = check_device(&dev))) return rc;
     const bool bf16 = out_dtype == GC_BF16;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int ctas = split_ctas(rows, cols, k);
+    if (ctas > 1) return launch_split(A, lda, a_scale, B, ldb, b_scale, rows, cols, k, bf16, out, ldo, ctas, dev_status, dev, st);
     const ImPlan pl = make_im_plan(rows, cols, k, bf16);
     ImParams p{};
     p.rows_m = pl.staged ? rows : cols;
@@ -772,7 +952,7 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n, units = sm_count() / (pl.pair ? 2 : 1);
     const dim3 grid((unsigned)std::min(total, units) * (pl.pair ? 2u : 1u));
     const cudaError_t e = launch_chained(kernels[2 * bf16 + 2 * pl.staged + pl.pair], grid, IM_THREADS, IM_SMEM,
-                                         pl.pair ? 2 : 1, static_cast<cudaStream_t>(cuda_stream), mm, mn, mo, p);
+                                         pl.pair ? 2 : 1, st, mm, mn, mo, p);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return GC_ERR_CUDA;

@@ -163,6 +163,9 @@ SHAPES = [
     (127, 640, 384), (128, 128, 1024), (129, 129, 129), (200, 3000, 96), (255, 255, 255), (256, 256, 256),
     (257, 300, 640), (300, 1, 768), (513, 1030, 2050), (1000, 777, 36), (1531, 2062, 768), (2048, 2048, 128), (4097, 40, 72),
     (8, 40, 16384), (300, 500, 8192),
+    # contractions shared by clusters of eight and of four, and just not
+    (1, 1, 2048), (1, 2304, 2048), (1, 2305, 2048), (1, 4736, 3000), (2, 4737, 2000), (16, 129, 1921), (16, 129, 1920),
+    (17, 2304, 4096), (17, 2305, 4096), (33, 500, 3969), (64, 100, 5000), (64, 100, 3968), (65, 100, 5000), (5, 131, 131071),
 ]
 
 
@@ -239,7 +242,7 @@ def test_outputs_beyond_32_bits(binding):
         assert torch.equal(out[r:r + 300], _product(A[r:r + 300], sa[r:r + 300], B, sb, F32))
 
 
-@pytest.mark.parametrize("rows,cols,k", [(1, 5000, 768), (600, 900, 256)])
+@pytest.mark.parametrize("rows,cols,k", [(1, 5000, 768), (600, 900, 256), (3, 200, 4096)])
 def test_captured_and_on_another_stream(binding, rows, cols, k):
     A, sa, B, sb = _operands(rows, cols, k, seed=4)
     x = torch.randn(rows, k, device="cuda")
