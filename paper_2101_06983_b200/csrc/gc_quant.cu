@@ -341,7 +341,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
     if (threadIdx.x == 0) {
         abort_s = 0;
         for (int s = 0; s < IM_MAX_ST; ++s) {
-            mbar_init(smem_u32(&bars.full[s]), 2);             // the two producer warps (pairs: the leader's)
+            mbar_init(smem_u32(&bars.full[s]), 1);             // the producer warp whose turn it is (pairs: the leader's)
             mbar_init(smem_u32(&bars.empty[s]), 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -380,28 +380,32 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
     };
 
     if (warp < NPROD) {
-        const bool is_m = warp == 0;       // warp 0: the M side, warp 1: the N side
-        const uint32_t bytes = is_m ? CHUNK_BYTES : (uint32_t)n_rows * 128u;
-        int stage = 0;
+        // the two warps take turns with the stages: one alone issues no more than 23 bytes a cycle
+        const uint32_t m_bytes = CHUNK_BYTES, n_bytes = (uint32_t)n_rows * 128u;
+        int stage = 0, item = 0;
         uint32_t phase = 0;
         bool ok = true;
         for (int64_t t = first; t < total && ok; t += by) {
             int tm, tn;
             tile_at(t, &tm, &tn);
-            const int row = is_m ? tm * M_ROWS + rank * 128 : tn * p.bn + rank * n_rows;
-            for (int kb = 0; kb < p.kblocks; ++kb) {
-                ok = mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag);
-                if (!ok) break;
-                const uint32_t full = smem_u32(&bars.full[stage]);
-                const uint32_t dst = smem + stage * stage_bytes + (is_m ? 0u : CHUNK_BYTES);
-                const uint32_t full_leader = PAIR ? mapa_u32(full, 0) : full;
-                if (elect_one()) {
-                    if (PAIR) {
-                        if (rank == 0) mbar_expect_tx(full, 2 * bytes);
-                        tma_load_2d_pair(dst, is_m ? &mapM : &mapN, kb * IM_KB, row, full_leader);
-                    } else {
-                        mbar_expect_tx(full, bytes);
-                        tma_load_2d(dst, is_m ? &mapM : &mapN, kb * IM_KB, row, full);
+            const int m_row = tm * M_ROWS + rank * 128, n_row = tn * p.bn + rank * n_rows;
+            for (int kb = 0; kb < p.kblocks; ++kb, ++item) {
+                if ((item & 1) == warp) {
+                    ok = mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag);
+                    if (!ok) break;
+                    const uint32_t full = smem_u32(&bars.full[stage]);
+                    const uint32_t dst = smem + stage * stage_bytes;
+                    const uint32_t full_leader = PAIR ? mapa_u32(full, 0) : full;
+                    if (elect_one()) {
+                        if (PAIR) {
+                            if (rank == 0) mbar_expect_tx(full, 2 * (m_bytes + n_bytes));
+                            tma_load_2d_pair(dst, &mapM, kb * IM_KB, m_row, full_leader);
+                            tma_load_2d_pair(dst + CHUNK_BYTES, &mapN, kb * IM_KB, n_row, full_leader);
+                        } else {
+                            mbar_expect_tx(full, m_bytes + n_bytes);
+                            tma_load_2d(dst, &mapM, kb * IM_KB, m_row, full);
+                            tma_load_2d(dst + CHUNK_BYTES, &mapN, kb * IM_KB, n_row, full);
+                        }
                     }
                 }
                 if (++stage == p.stages) { stage = 0; phase ^= 1u; }
