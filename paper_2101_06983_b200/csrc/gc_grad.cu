@@ -42,18 +42,18 @@ struct Entry {
     int64_t units;        // FLAT_VEC, ROWS_VEC: whole vectors; ELEM: elements
     int64_t ld, ld_out;   // elements
     uint32_t cols;        // ROWS_VEC: vectors of a row; ELEM: elements of a row
-    uint32_t first;       // its first tile
     uint16_t mode;
     uint16_t bf16;
     uint16_t head, tail;  // FLAT_VEC: single elements before and after the vectors
 };
 template <int N>
 struct List {
-    Entry e[N];
     int n;
     uint32_t tiles;
+    uint32_t first[N];    // first tile of each entry: side by side, for the search
+    Entry e[N];
 };
-constexpr int FEW = 32, SOME = 224, MANY = 580;        // 32,764 bytes of parameters at most; fewer are copied faster
+constexpr int FEW = 32, SOME = 224, MANY = 540;        // 32,764 bytes of parameters at most; fewer are copied faster
 static_assert(sizeof(List<MANY>) <= 32600, "kernel parameters");
 
 __device__ __forceinline__ float2 widen(uint32_t w) {
@@ -125,17 +125,17 @@ template <int N>
 __device__ __forceinline__ int entry_of(const List<N>& list, uint32_t t, int lo, int hi) {
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (list.e[mid].first <= t) lo = mid; else hi = mid - 1;
+        if (list.first[mid] <= t) lo = mid; else hi = mid - 1;
     }
     return lo;
 }
-// A tile of an entry that is no stretch of vectors: its first unit and where that lies.
+// Tile t of an entry that is no stretch of vectors: its first unit and where that lies.
 struct Tile {
     int64_t r;
     uint32_t c, n;        // row and column of the first unit; units of the tile
 };
 __device__ __forceinline__ Tile tile_of(const Entry& e, uint32_t t) {
-    const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS;
+    const int64_t u = (int64_t)t * GR_TILE_UNITS;
     Tile x;
     x.n = (uint32_t)min((int64_t)GR_TILE_UNITS, e.units - u);
     x.r = u / e.cols;
@@ -167,7 +167,7 @@ __device__ __forceinline__ double squares_of(const Entry& e, uint32_t t, int tid
     const bool bf16 = e.bf16;
     uint4 v[GR_PER];
     if (e.mode == FLAT_VEC) {
-        const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + tid;
+        const int64_t u = (int64_t)t * GR_TILE_UNITS + tid;
         const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4) + 16 * u;
         if (u - tid + GR_TILE_UNITS <= e.units) {
 #pragma unroll
@@ -179,7 +179,7 @@ __device__ __forceinline__ double squares_of(const Entry& e, uint32_t t, int tid
                                                     : make_uint4(0, 0, 0, 0);
         }
         double sum = square_sum(v, bf16);
-        if (t == e.first && tid < e.head + e.tail) {
+        if (t == 0 && tid < e.head + e.tail) {
             const double x = load_one(e.src, tid < e.head ? tid : tid + e.units * (bf16 ? 8 : 4), bf16);
             sum = fma(x, x, sum);
         }
@@ -212,7 +212,7 @@ __device__ __forceinline__ void scale_tile(const Entry& e, uint32_t t, int tid, 
     const bool bf16 = e.bf16;
     if (copy && e.src == e.dst) return;                  // the values stay as they are
     if (e.mode == FLAT_VEC) {
-        const int64_t u = (int64_t)(t - e.first) * GR_TILE_UNITS + tid;
+        const int64_t u = (int64_t)t * GR_TILE_UNITS + tid;
         const char* src = static_cast<const char*>(e.src) + e.head * (bf16 ? 2 : 4) + 16 * u;
         char* dst = static_cast<char*>(e.dst) + e.head * (bf16 ? 2 : 4) + 16 * u;
         if (u - tid + GR_TILE_UNITS <= e.units) {
@@ -230,7 +230,7 @@ __device__ __forceinline__ void scale_tile(const Entry& e, uint32_t t, int tid, 
                     *reinterpret_cast<uint4*>(dst + 16 * GR_THREADS * i) = copy ? v : scale_vec(v, bf16, c);
                 }
         }
-        if (t == e.first && tid < e.head + e.tail) {
+        if (t == 0 && tid < e.head + e.tail) {
             const int64_t i = tid < e.head ? tid : tid + e.units * (bf16 ? 8 : 4);
             scale_one(e, i, i, copy, c);
         }
@@ -263,7 +263,7 @@ grad_square_kernel(const __grid_constant__ List<N> list, double* part) {
     int at = 0;
     for (uint32_t t = blockIdx.x; t < list.tiles; t += gridDim.x) {
         at = entry_of(list, t, at, list.n - 1);
-        sum += squares_of(list.e[at], t, threadIdx.x);
+        sum += squares_of(list.e[at], t - list.first[at], threadIdx.x);
     }
     sum = block_sum(sum, warp_part);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -315,7 +315,7 @@ grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int 
     for (int64_t back = (int64_t)list.tiles - 1 - blockIdx.x; back >= 0; back -= gridDim.x) {
         const uint32_t t = (uint32_t)back;
         at = entry_of(list, t, 0, at);
-        scale_tile(list.e[at], t, threadIdx.x, copy, c);
+        scale_tile(list.e[at], t - list.first[at], threadIdx.x, copy, c);
     }
 }
 
@@ -335,7 +335,7 @@ grad_cluster_kernel(const __grid_constant__ List<N> list, float max_norm, double
     int at = 0;
     for (uint32_t t = first; t < list.tiles; t += by) {
         at = entry_of(list, t, at, list.n - 1);
-        sum += squares_of(list.e[at], t, tid);
+        sum += squares_of(list.e[at], t - list.first[at], tid);
     }
     sum = block_sum(sum, warp_part);
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");                // and so have those it sends to
@@ -355,7 +355,7 @@ grad_cluster_kernel(const __grid_constant__ List<N> list, float max_norm, double
     const float c = factor_of(total, max_norm, &copy);
     for (uint32_t t = first; t < list.tiles; t += by) {
         at = entry_of(list, t, 0, list.n - 1);
-        scale_tile(list.e[at], t, tid, copy, c);
+        scale_tile(list.e[at], t - list.first[at], tid, copy, c);
     }
 }
 
@@ -496,7 +496,7 @@ int next_group(const gc_tensor* list, int64_t n, bool write, int64_t* i, List<MA
             if (l.n == 0) return GC_ERR_LIMIT;
             break;
         }
-        e.first = (uint32_t)tiles;
+        l.first[l.n] = (uint32_t)tiles;
         tiles += more;
         l.e[l.n++] = e;
     }
@@ -508,6 +508,7 @@ template <int N, typename Go>
 cudaError_t with_size(const List<MANY>& l, Go go) {
     List<N> x;
     std::copy(l.e, l.e + l.n, x.e);
+    std::copy(l.first, l.first + l.n, x.first);
     x.n = l.n;
     x.tiles = l.tiles;
     return go(x);
