@@ -108,7 +108,7 @@ __device__ __forceinline__ uint2 to_i8(const Piece<BF16>& x, float inv, float sc
 // 1 / s within 2^-22 of itself.  bf16 rows: on the side of it that s = amax / 127 (1 - eps) is off to.  Such rows are full
 // of values with 127 x / amax = h halfway between two integers: x / s is then h (1 + eps), and x * inv = h (1 + eps) s inv lies
 // on the same side of h if s inv - 1 is not of the other sign.  Without this nearly every piece of a warp has a
-// value whose first integer is wrong (131072 x 768: 61 us, with it 55).
+// value whose first integer is wrong (131072 x 768, a warp to a row: 61 us, with it 55).
 template <bool BF16>
 __device__ __forceinline__ float reciprocal(float s, float amax) {
     float inv;
@@ -886,7 +886,15 @@ int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dt
 #define GC_QZ(LANES, KEEP)                                                      \
     (dtype == GC_BF16 ? go(quantize_rows_kernel<true, LANES, KEEP>, QZ_THREADS / LANES) \
                       : go(quantize_rows_kernel<false, LANES, KEEP>, QZ_THREADS / LANES))
-    if (d <= 64) e = GC_QZ(8, 1);
+    // Many bf16 rows: fewer lanes to a row share what a row costs whatever its width (its maximum's exchange, 1 / s, addresses).
+    // Measured, us, as fewer rows take them / as many: 131072 x 768 55 / 52, 100000 x 256 18.4 / 15.4, 32768 x 512 12.4 / 11.3;
+    // 16384 x 768 9.1 / 9.9, 4096 x 768 3.1 / 4.5.
+    const bool many = dtype == GC_BF16 && rows >= 128 * (int64_t)sm_count();
+#define GC_QZ_MANY(LANES, KEEP) go(quantize_rows_kernel<true, LANES, KEEP>, QZ_THREADS / LANES)
+    if (many && d > 128 && d <= 256) e = GC_QZ_MANY(8, 4);
+    else if (many && d > 256 && d <= 512) e = GC_QZ_MANY(16, 4);
+    else if (many && d > 512 && d <= 768) e = GC_QZ_MANY(16, 6);
+    else if (d <= 64) e = GC_QZ(8, 1);
     else if (d <= 128) e = GC_QZ(8, 2);
     else if (d <= 256) e = GC_QZ(16, 2);
     else if (d <= 512) e = GC_QZ(32, 2);
@@ -896,6 +904,7 @@ int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dt
     else if (d <= 4096) e = GC_QZ(128, 4);
     else e = GC_QZ(256, 4);
 #undef GC_QZ
+#undef GC_QZ_MANY
     if (e != cudaSuccess) {
         cudaGetLastError();
         return GC_ERR_CUDA;

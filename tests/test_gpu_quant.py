@@ -61,7 +61,8 @@ def _check_quantize(binding, x, pad=0):
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("rows,d", [(1, 1), (1, 768), (3, 15), (5, 16), (7, 17), (9, 31), (33, 500), (8, 512), (300, 513),
                                     (1, 4096), (2, 1024), (17, 1025), (640, 768), (4, 8191), (3, 8192), (5, 8193),
-                                    (2, 20011), (5000, 64)])
+                                    (2, 20011), (5000, 64), (20000, 129), (19000, 256), (19000, 257), (18944, 512), (18945, 513),
+                                    (19001, 768), (18944, 769)])
 def test_rows(binding, rows, d, dtype):
     gen = torch.Generator(device="cuda").manual_seed(rows * 7 + d)
     unit = 8 if dtype == BF else 4
