@@ -53,7 +53,7 @@ struct List {
     uint32_t first[N];    // first tile of each entry: side by side, for the search
     Entry e[N];
 };
-constexpr int FEW = 32, SOME = 224, MANY = 540;        // 32,764 bytes of parameters at most; fewer are copied faster
+constexpr int FEW = 32, SOME = 96, MORE = 224, MANY = 540;        // 32,764 bytes of parameters at most; fewer are copied faster
 static_assert(sizeof(List<MANY>) <= 32600, "kernel parameters");
 
 __device__ __forceinline__ float2 widen(uint32_t w) {
@@ -401,27 +401,58 @@ bool apart_by_columns(const gc_tensor& a, uintptr_t a_lo, int64_t a_ld, const gc
     return off >= a.cols * ea && off + b.cols * eb <= pitch;
 }
 
+// Spans that come in ascending order, in a few strands that lie apart (tensors of flat buffers, one for each type, and
+// their outputs): no two of them meet.  The usual list, told without sorting it.
+struct Strands {
+    static constexpr int MOST = 8;
+    static constexpr uintptr_t NEAR = 1 << 16;
+    uintptr_t lo[MOST], hi[MOST];
+    int n = 0;
+    bool good = true;
+    void add(uintptr_t a, uintptr_t b) {
+        for (int k = 0; k < n; ++k)
+            if (a >= hi[k] && a - hi[k] < NEAR) {
+                hi[k] = b;
+                return;
+            }
+        if (n == MOST) { good = false; return; }
+        lo[n] = a;
+        hi[n++] = b;
+    }
+    bool apart() const {
+        for (int i = 0; i < n && good; ++i)
+            for (int k = 0; k < i; ++k)
+                if (lo[i] < hi[k] && lo[k] < hi[i]) return false;
+        return good;
+    }
+};
 // No place that is written may be read or written through another tensor of the list.
 int check_overlap(const gc_tensor* list, int64_t n) {
-    std::vector<Span> s;
-    s.reserve((size_t)n * 2);
-    bool sorted = true;
-    auto add = [&](uintptr_t lo, uintptr_t len, int64_t i, bool written) {
-        if (!s.empty() && lo < s.back().hi) sorted = false;
-        s.push_back({lo, lo + len, (int)i, written});
-    };
+    Strands strands;
+    bool elsewhere = false;
     for (int64_t i = 0; i < n; ++i)
         if (list[i].rows > 0 && list[i].cols > 0) {
             const gc_tensor& t = list[i];
-            const uintptr_t lo = (uintptr_t)t.data;
             const bool in_place = !t.out || t.out == t.data;
             if (in_place && t.out && t.rows > 1 && t.ld_out != t.ld) return GC_ERR_ALIAS;
-            add(lo, bytes_of(t, t.ld), i, in_place);
+            if (strands.good) {
+                const uintptr_t lo = (uintptr_t)t.data;
+                strands.add(lo, lo + bytes_of(t, t.ld));
+                if (!in_place) strands.add((uintptr_t)t.out, (uintptr_t)t.out + bytes_of(t, t.ld_out));
+            }
+            elsewhere |= !in_place;
         }
+    if (strands.apart()) return GC_OK;
+    std::vector<Span> s;
+    s.reserve((size_t)n * (elsewhere ? 2 : 1));
     for (int64_t i = 0; i < n; ++i)
-        if (list[i].rows > 0 && list[i].cols > 0 && list[i].out && list[i].out != list[i].data)
-            add((uintptr_t)list[i].out, bytes_of(list[i], list[i].ld_out), i, true);
-    if (sorted) return GC_OK;
+        if (list[i].rows > 0 && list[i].cols > 0) {
+            const gc_tensor& t = list[i];
+            const uintptr_t lo = (uintptr_t)t.data, out = (uintptr_t)t.out;
+            const bool in_place = !t.out || t.out == t.data;
+            s.push_back({lo, lo + bytes_of(t, t.ld), (int)i, in_place});
+            if (!in_place) s.push_back({out, out + bytes_of(t, t.ld_out), (int)i, true});
+        }
     std::sort(s.begin(), s.end(), [](const Span& a, const Span& b) { return a.lo < b.lo; });
     auto pitch = [&](const Span& x) {
         const gc_tensor& t = list[x.entry];
@@ -515,7 +546,8 @@ cudaError_t with_size(const List<MANY>& l, Go go) {
 }
 template <typename Go>
 int with_list(const List<MANY>& l, Go go) {
-    const cudaError_t e = l.n <= FEW ? with_size<FEW>(l, go) : l.n <= SOME ? with_size<SOME>(l, go) : go(l);
+    const cudaError_t e = l.n <= FEW ? with_size<FEW>(l, go) : l.n <= SOME ? with_size<SOME>(l, go)
+                          : l.n <= MORE ? with_size<MORE>(l, go) : go(l);
     if (e == cudaSuccess) return GC_OK;
     cudaGetLastError();
     return GC_ERR_CUDA;

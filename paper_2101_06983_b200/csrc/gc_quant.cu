@@ -19,7 +19,7 @@ namespace {
 // Rows to 8 bits
 // ---------------------------------------------------------------------------------------------------
 constexpr int QZ_THREADS = 256;
-constexpr int QZ_BLOCKS = 4;                // to an SM: 3 and 5 are 5 to 20 % slower for nearly all widths
+constexpr int QZ_BLOCKS = 4;               // to an SM: 3 and 5 are 4 to 20 % slower for nearly all widths
 constexpr float MAGIC = 12582912.f;        // 1.5 * 2^23: adding it rounds to an integer, left in the low bits
 
 constexpr float RECIP_127 = 1.f / 127.f;   // rounded to fp32
@@ -65,11 +65,12 @@ if (BF16) {
         return m;
     }
 };
-// The 8-bit integers of a piece.  r, x * inv rounded to an integer, is the nearest one to x / scale if the remainder
-// x - r scale is below half a scale.  The remainder is exact (one fused multiply-add: x * inv misses the
-// quotient by less than 2^-15, and the difference has no bits below half of scale's last), so where one of the eight
-// is that large, comparing it with scale / 2 decides.  Rows of scales below 2^-100, whose 1 / s may be infinite, form
-// the quotients in fp64.
+// The 8-bit integers of a piece: x * inv rounded to integers, r.
+// fp32 rows: r is the nearest integer to x / scale if the remainder x - r scale is below half a scale.  The remainder is
+// exact (one fused multiply-add: x * inv misses the quotient by less than 2^-15, and the difference has no bits below half of
+// scale's last), so where one of the eight is that large, comparing it with scale / 2 decides.
+// bf16 rows: see reciprocal().  Rows that neither serves (scales below 2^-100, whose 1 / s may be infinite) form the
+// quotients in fp64.
 __device__ __noinline__ uint32_t exact_i8(float x, float scale) {
     const double q = rint((double)x / (double)scale);
     return (uint32_t)(int)fmin(fmax(q, -127.0), 127.0);
@@ -84,8 +85,10 @@ __device__ __forceinline__ uint2 to_i8(const Piece<BF16>& x, float inv, float sc
     for (int e = 0; e < 8; e += 2) {
         const uint64_t v = pack2(x.at(e), x.at(e + 1)), t = fma2(v, inv2, magic2);
         float a, b;
-        unpack2(fma2(fma2(t, minus2, magic2), scale2, v), a, b);
-        most = fmaxf(most, fmaxf(fabsf(a), fabsf(b)));
+        if (!BF16) {
+            unpack2(fma2(fma2(t, minus2, magic2), scale2, v), a, b);
+            most = fmaxf(most, fmaxf(fabsf(a), fabsf(b)));
+        }
         unpack2(t, a, b);
         m[e] = __float_as_uint(a);
         m[e + 1] = __float_as_uint(b);
@@ -93,7 +96,7 @@ __device__ __forceinline__ uint2 to_i8(const Piece<BF16>& x, float inv, float sc
     if (wide) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) m[e] = exact_i8(x.at(e), scale);
-    } else if (most >= 0.5f * scale) {
+    } else if (!BF16 && most >= 0.5f * scale) {
         const float half = 0.5f * scale;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -105,18 +108,27 @@ __device__ __forceinline__ uint2 to_i8(const Piece<BF16>& x, float inv, float sc
                       __byte_perm(__byte_perm(m[4], m[5], 0x0040), __byte_perm(m[6], m[7], 0x0040), 0x5410));
 }
 
-// 1 / s within 2^-22 of itself.  bf16 rows: on the side of it that s = amax / 127 (1 - eps) is off to.  Such rows are full
-// of values with 127 x / amax = h halfway between two integers: x / s is then h (1 + eps), and x * inv = h (1 + eps) s inv lies
-// on the same side of h if s inv - 1 is not of the other sign.  Without this nearly every piece of a warp has a
-// value whose first integer is wrong (131072 x 768, a warp to a row: 61 us, with it 55).
+// inv, 1 / s within 2^-21 of itself; false where the row has to form its quotients in fp64.
+// bf16 rows: x = X 2^a and amax = A 2^b with integers X, A below 256, so 127 x / amax lies either halfway between two
+// integers or at least 2^-16 of itself away from there, while x / s and x * inv miss it by less than 2^-20.  So x * inv rounds
+// as x / s does unless 127 x / amax = h is such a half.  Then x / s = h (amax / 127 s) and x * inv = h (amax inv / 127), and inv is
+// moved until both factors are on the same side of 1, or both are 1 (ties to even: one rounding, of the fused
+// multiply-add).  Two differences with exact signs for a row replace a remainder for every value, of which nearly
+// every piece of a warp has one to look at (131072 x 768: 61 us with that, a warp to a row).
 template <bool BF16>
-__device__ __forceinline__ float reciprocal(float s, float amax) {
-    float inv;
+__device__ __forceinline__ bool reciprocal(float s, float amax, float& inv) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
-    if (!BF16) return inv;
-    const float eps = fmaf(-127.f, s, amax), off = fmaf(s, inv, -1.f);
-    const uint32_t step = eps > 0.f && off < 0.f ? 1u : eps < 0.f && off > 0.f ? 0xffffffffu : 0u;
-    return __uint_as_float(__float_as_uint(inv) + step);
+    if (!BF16) return true;
+    const float eps = fmaf(-127.f, s, amax);
+    auto side = [&] { return fmaf(amax, inv, -127.f); };
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float at = side();
+        if (eps > 0.f && at <= 0.f) inv = __uint_as_float(__float_as_uint(inv) + 1u);
+        if (eps < 0.f && at >= 0.f) inv = __uint_as_float(__float_as_uint(inv) - 1u);
+    }
+    const float at = side();
+    return eps > 0.f ? at > 0.f : eps < 0.f ? at < 0.f : at == 0.f;
 }
 
 // LANES lanes (8, 16, a warp or several) to a row; a lane holds KEEP pieces of 8 values of it in registers and reads
@@ -165,8 +177,8 @@ quantize_rows_kernel(const void* X, int64_t ldx, int64_t rows, int64_t d, int8_t
         const bool bad = most >= 0x7f800000u;
         const float s = bad ? __uint_as_float(0x7fc00000u) : __uint_as_float(most) * RECIP_127;
         const bool none = bad || s == 0.f;
-        const bool wide = s < 0x1p-100f;   // 1 / s may be infinite, s itself of few bits
-        const float inv = none || wide ? 0.f : reciprocal<BF16>(s, __uint_as_float(most));
+        float inv = 0.f;
+        const bool wide = s < 0x1p-100f || (!none && !reciprocal<BF16>(s, __uint_as_float(most), inv));
         if (!live) continue;
         if (lane == 0) scale[i] = s;
         int8_t* dst = q + i * ldq;
@@ -911,9 +923,9 @@ int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dt
     (dtype == GC_BF16 ? go(quantize_rows_kernel<true, LANES, KEEP>, QZ_THREADS / LANES) \
                       : go(quantize_rows_kernel<false, LANES, KEEP>, QZ_THREADS / LANES))
     // Many bf16 rows: fewer lanes to a row share what a row costs whatever its width (its maximum's exchange, 1 / s, addresses).
-    // Measured, us, as fewer rows take them / as many: 131072 x 768 55 / 52, 100000 x 256 18.4 / 15.4, 32768 x 512 12.4 / 11.3;
-    // 16384 x 768 9.1 / 9.9, 4096 x 768 3.1 / 4.5.
-    const bool many = dtype == GC_BF16 && rows >= 128 * (int64_t)sm_count();
+    // Measured, us, as fewer rows take them / as many: 131072 x 768 53.5 / 48.5, 100000 x 256 17.6 / 15.6, 32768 x 512 11.9 / 10.4,
+    // 8192 x 768 4.2 / 4.1; 4096 x 768 2.9 / 3.6.
+    const bool many = dtype == GC_BF16 && rows >= 48 * (int64_t)sm_count();
 #define GC_QZ_MANY(LANES, KEEP) go(quantize_rows_kernel<true, LANES, KEEP>, QZ_THREADS / LANES)
     if (many && d > 128 && d <= 256) e = GC_QZ_MANY(8, 4);
     else if (many && d > 256 && d <= 512) e = GC_QZ_MANY(16, 4);

@@ -174,7 +174,7 @@ def test_orders_of_dimensions(binding):
     assert torch.equal(a.cpu(), _scaled(before[0], c)) and torch.equal(b.cpu(), _scaled(before[1], c))
 
 
-@pytest.mark.parametrize("n", [31, 32, 33, 40, 223, 224, 225, 539, 540, 541, 580, 1400])
+@pytest.mark.parametrize("n", [31, 32, 33, 40, 95, 96, 97, 223, 224, 225, 539, 540, 541, 580, 1400])
 def test_lists_of_many_tensors(binding, n):
     """More tensors than one launch takes."""
     sizes = [(i * 37) % 200 + (5000 if i % 101 == 0 else 0) for i in range(n)]

@@ -61,8 +61,8 @@ def _check_quantize(binding, x, pad=0):
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("rows,d", [(1, 1), (1, 768), (3, 15), (5, 16), (7, 17), (9, 31), (33, 500), (8, 512), (300, 513),
                                     (1, 4096), (2, 1024), (17, 1025), (640, 768), (4, 8191), (3, 8192), (5, 8193),
-                                    (2, 20011), (5000, 64), (20000, 129), (19000, 256), (19000, 257), (18944, 512), (18945, 513),
-                                    (19001, 768), (18944, 769)])
+                                    (2, 20011), (5000, 64), (7104, 129), (7111, 256), (7200, 257), (7103, 512), (7104, 512),
+                                    (7105, 513), (7333, 768), (7120, 769)])
 def test_rows(binding, rows, d, dtype):
     gen = torch.Generator(device="cuda").manual_seed(rows * 7 + d)
     unit = 8 if dtype == BF else 4
@@ -90,6 +90,25 @@ def test_values_next_to_borders(binding, d, dtype):
     _, xs = _padded(rows, d, dtype, 8, 0.0)
     xs.copy_(torch.from_numpy(x).cuda())
     _check_quantize(binding, xs)
+
+
+def test_every_bf16_quotient(binding):
+    """Every mantissa of a row's largest value against every bf16 value down to 2^-10 of it, both signs, at exponents from
+    the smallest that have an fp32 reciprocal to the largest."""
+    mant = torch.arange(128, 256, dtype=torch.float64)
+    rows = []
+    for e in (-98, -30, -7, 0, 1, 60, 110):
+        for a in mant:
+            top = a * 2.0 ** (e - 7)
+            x = torch.cat([mant * 2.0 ** (e - 7 - j) for j in range(11)])
+            x = x[x <= top]
+            row = torch.zeros(2 * 11 * 128, dtype=torch.float64)
+            row[:len(x)], row[len(row) // 2:len(row) // 2 + len(x)] = x, -x
+            rows.append(row)
+    x = torch.stack(rows).to(BF)
+    assert torch.equal(x.double(), torch.stack(rows))
+    _check_quantize(binding, x.cuda())
+    _check_quantize(binding, x.cuda()[:, :1408].contiguous()[:, 700:1212].contiguous().repeat(25, 1))
 
 
 def test_exact_ties(binding):
