@@ -262,6 +262,27 @@ def test_outputs_beyond_32_bits(binding):
         assert torch.equal(out[r:r + 300], _product(A[r:r + 300], sa[r:r + 300], B, sb, F32))
 
 
+def test_inputs_beyond_32_bits(binding):
+    """An index of more than 2^32 bytes, made from bf16 rows of more, at its far end; one query against it."""
+    n, d = 6_000_000, 768
+    x = torch.zeros(n, d, dtype=BF, device="cuda")
+    x[-5000:] = torch.randn(5000, d, device="cuda")
+    x[n // 2 - 500:n // 2 + 500] = torch.randn(1000, d, device="cuda")
+    q, s = torch.full((n, d), 99, dtype=torch.int8, device="cuda"), torch.full((n,), -1.0, device="cuda")
+    binding.gc_quantize_rows(x, q, s)
+    for part in (slice(n - 5000, n), slice(n // 2 - 500, n // 2 + 500), slice(0, 1000)):
+        want_q, want_s = _quantized(x[part])
+        assert torch.equal(q[part].cpu(), want_q) and torch.equal(s[part].cpu(), want_s)
+    del x
+    for rows in (1, 70):
+        A, sa, _, _ = _operands(rows, 1, d, seed=rows)
+        out = torch.full((rows, n), -1.0, device="cuda")
+        binding.gc_matmul_i8(A, sa, q, s, out)
+        for part in (slice(n - 5000, n), slice(n // 2 - 500, n // 2 + 500), slice(0, 1000)):
+            assert torch.equal(out[:, part], _product(A, sa, q[part], s[part], F32))
+        del out
+
+
 @pytest.mark.parametrize("rows,cols,k", [(1, 5000, 768), (600, 900, 256), (3, 200, 4096)])
 def test_captured_and_on_another_stream(binding, rows, cols, k):
     A, sa, B, sb = _operands(rows, cols, k, seed=4)
