@@ -499,6 +499,7 @@ class GradList:
             raise ValueError("out must hold one tensor for each gradient")
         self.n = len(self.grads)
         self.tensors = (_Tensor * max(self.n, 1))()
+        self.address = ctypes.addressof(self.tensors)
         self.device = self.grads[0].device if self.grads else None
         for i, g in enumerate(self.grads):
             o = None if self.out is None else self.out[i]
@@ -543,7 +544,7 @@ def gc_grad_norm(grads, norm=None, sq_sum=None, ws=None, dev_status=None) -> Non
     grads, dev = _grad_args(grads, ws, norm, sq_sum, dev_status)
     if ws is None:
         ws = _grad_ws(grads, dev)
-    rc = _lib.gc_grad_norm(grads.tensors, grads.n, _ptr(sq_sum), _ptr(norm), ws.data_ptr(), ws.numel(),
+    rc = _lib.gc_grad_norm(grads.address, grads.n, _ptr(sq_sum), _ptr(norm), ws.data_ptr(), ws.numel(),
                            _ptr(dev_status), _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_grad_norm")
@@ -554,7 +555,7 @@ def gc_grad_scale(grads, sq_sum, max_norm, dev_status=None) -> None:
     sq_sum[0] (float64): of gc_grad_norm, or summed over ranks that hold different gradients."""
     _scalar(sq_sum, torch.float64, "sq_sum")
     grads, dev = _grad_args(grads, None, sq_sum, dev_status)
-    rc = _lib.gc_grad_scale(grads.tensors, grads.n, _ptr(sq_sum), max_norm, _ptr(dev_status),
+    rc = _lib.gc_grad_scale(grads.address, grads.n, _ptr(sq_sum), max_norm, _ptr(dev_status),
                             _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_grad_scale")
@@ -569,7 +570,7 @@ def gc_grad_clip(grads, max_norm, norm, sq_sum=None, ws=None, dev_status=None) -
     grads, dev = _grad_args(grads, ws, norm, sq_sum, dev_status)
     if ws is None:
         ws = _grad_ws(grads, dev)
-    rc = _lib.gc_grad_clip(grads.tensors, grads.n, max_norm, _ptr(sq_sum), _ptr(norm), ws.data_ptr(),
+    rc = _lib.gc_grad_clip(grads.address, grads.n, max_norm, _ptr(sq_sum), _ptr(norm), ws.data_ptr(),
                            ws.numel(), _ptr(dev_status), _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_grad_clip")

@@ -86,6 +86,41 @@ def test_places_that_two_tensors_share(binding):
     assert _clip(binding, dict(rows=1, cols=1 << 12), dict(data=0x20000), dict(data=0x10000 + 4 * 2000)) == ALIAS
 
 
+def _flats(n, gap=0):
+    """Tensors of two flat buffers in turn, each with an output in another buffer."""
+    at = {k: v for k, v in enumerate((0x10000000, 0x20000000, 0x30000000, 0x40000000))}
+    out = []
+    for i in range(n):
+        size = 4 * (i % 7 + 1) * 5
+        out.append(dict(data=at[i % 2], out=at[2 + i % 2], rows=1, cols=size // 4, ld=0, ld_out=0))
+        at[i % 2] += size + gap
+        at[2 + i % 2] += size + gap
+    return out
+
+
+@pytest.mark.parametrize("n,gap", [(40, 0), (200, 512), (30, 1 << 17)])
+def test_shared_places_in_long_lists(binding, n, gap):
+    """One output moved onto another, onto a source, or onto itself: in strands, and in no order at all."""
+    import random
+    for order in (0, 1):
+        tensors = _flats(n, gap)
+        if order:
+            random.Random(n).shuffle(tensors)
+        for a, b, key in ((3, n - 2, "out"), (n - 1, 0, "data"), (n // 2, n // 2, "data")):
+            bad = [dict(t) for t in tensors]
+            bad[a]["out"] = tensors[b][key] + (4 if a == b else 0)
+            assert _clip(binding, *bad) == ALIAS
+        # two sources may share a place, but not with their gradients scaled where they lie
+        twice = [dict(t) for t in tensors]
+        twice[1]["data"] = twice[2]["data"]
+        if torch.cuda.is_available():
+            continue                                     # the addresses are not real ones
+        assert _passes(_clip(binding, *tensors))
+        assert _passes(_clip(binding, *twice))
+        assert _passes(_clip(binding, *[dict(t, out=None) for t in tensors]))
+        assert _clip(binding, *[dict(t, out=None) for t in twice]) == ALIAS
+
+
 @needs_no_gpu
 def test_lists_that_are_taken(binding):
     assert _passes(_clip(binding))
