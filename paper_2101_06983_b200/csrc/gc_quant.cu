@@ -7,7 +7,7 @@
 // bf16 48.4 us, 6.25 TB/s.
 // gc_matmul_i8 runs on the tensor cores (tcgen05, kind::i8: exact products and 32-bit integer sums).  Long contractions
 // are bound by the products (16384 x 768 x 4096 37 us, 2.8 POP/s; 8192 x 8192 x 4096 163 us, 3.4), short ones by the stores of the
-// result (4096 x 8192 x 768 to fp32 31 us, of which 134 MB take 20.5), few rows of A by reading B (1 x 131072 x 768 18.7 us,
+// result (4096 x 8192 x 768 to fp32 31 us, of which 134 MB take 20.5; to bf16 24), few rows of A by reading B (1 x 131072 x 768 18.7 us,
 // 5.4 TB/s).
 #include <cuda_bf16.h>
 #include <math.h>
@@ -224,9 +224,10 @@ constexpr uint32_t IM_SCALES = 256;        // bytes of a warp: the scales of its
 // N side (bn to a tile) its columns.
 //   plain      M: B (channels), N: A (tokens).  32 lanes hold neighbouring outputs and store them as they are.  Few rows
 //              of A cost no more than their share of the instruction.
-//   staged     bf16 outputs only.  M: A, N: B.  A lane holds neighbouring outputs of a row; blocks of 32 rows x 64
+//   staged     bf16 outputs only.  M: A, N: B.  A lane holds neighbouring outputs of a row; blocks of 32 rows x 32
 //              columns leave through shared memory with bulk tensor stores: half the words to shared memory that
-//              fp32 would take, and no trading of rows between lanes.
+//              fp32 would take, and no trading of rows between lanes.  (Blocks of 64 columns take twice the buffers,
+//              which cost a stage of the ring: 4096 x 8192 x 768 27.2 us against 24.3.)
 struct ImParams {
     int64_t rows_m, rows_n;
     int kblocks;
@@ -338,11 +339,11 @@ __device__ __forceinline__ void store_block(const uint32_t (&v)[G], uint32_t sca
     }
 }
 
-// Bulk tensor loads with a cache policy.
-__device__ __forceinline__ uint64_t l2_policy(bool once) {
+// Bulk tensor load of rows that leave the L2 first.  (Only for rows that one CTA reads: a load with a policy, be it the
+// normal one, of rows that all CTAs read at once took 2500 x 50 x 2000 from 7.5 to 18.3 us.)
+__device__ __forceinline__ uint64_t evict_first() {
     uint64_t p;
-    if (once) asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
-    else      asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
 template <bool PAIR>
@@ -421,7 +422,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
 
     if (warp < NPROD) {
         // the two warps take turns with the stages: one alone issues no more than 23 bytes a cycle
-        const uint64_t policy = l2_policy(p.once != 0);
+        const uint64_t policy = evict_first();
         const uint32_t m_bytes = CHUNK_BYTES, n_bytes = (uint32_t)n_rows * 128u;
         int stage = 0, item = 0;
         uint32_t phase = 0;
@@ -440,11 +441,13 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
                     if (elect_one()) {
                         if (PAIR) {
                             if (rank == 0) mbar_expect_tx(full, 2 * (m_bytes + n_bytes));
-                            tma_load_policy<true>(dst, &mapM, kb * IM_KB, m_row, full_leader, policy);
+                            if (p.once) tma_load_policy<true>(dst, &mapM, kb * IM_KB, m_row, full_leader, policy);
+                            else        tma_load_2d_pair(dst, &mapM, kb * IM_KB, m_row, full_leader);
                             tma_load_2d_pair(dst + CHUNK_BYTES, &mapN, kb * IM_KB, n_row, full_leader);
                         } else {
                             mbar_expect_tx(full, m_bytes + n_bytes);
-                            tma_load_policy<false>(dst, &mapM, kb * IM_KB, m_row, full, policy);
+                            if (p.once) tma_load_policy<false>(dst, &mapM, kb * IM_KB, m_row, full, policy);
+                            else        tma_load_2d(dst, &mapM, kb * IM_KB, m_row, full);
                             tma_load_2d(dst + CHUNK_BYTES, &mapN, kb * IM_KB, n_row, full);
                         }
                     }
@@ -506,7 +509,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
         const int q = warp & 3, ew = warp - (NPROD + 1), group = ew >> 2;
         const int block = STAGED ? 64 : p.bn >= 64 ? 32 : 16;
         const uint32_t after = smem + p.stages * stage_bytes;
-        const uint32_t scales = after + (uint32_t)ew * IM_SCALES, buf = after + IM_EPI * IM_SCALES + (uint32_t)ew * 4096u;
+        const uint32_t scales = after + (uint32_t)ew * IM_SCALES, buf = after + IM_EPI * IM_SCALES + (uint32_t)ew * 2048u;
         float next_m = 0.f, next_n[2] = {0.f, 0.f};
         // the scales of a tile's rows and of this warp's columns of it, block after block
         auto fetch = [&](int64_t t) {
@@ -560,13 +563,13 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
             if (STAGED) {
                 const int c0 = group * 64;
                 if (c0 >= n) continue;
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                __syncwarp();
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {                                // 32 columns each
                     const int c = c0 + 32 * y;
                     float f[32];
                     scale_sums<32, true>(v[y], scales + 128 * y, mine, f);
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
                     if (j0 + c + 32 > p.whole && p.whole < p.rows_n && i < p.rows_m) {
                         // the columns after the last whole 16 bytes
 #pragma unroll
@@ -576,7 +579,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
                                 static_cast<__nv_bfloat16*>(p.out)[i * p.ldo + j] = __float2bfloat16_rn(f[e]);
                         }
                     }
-                    // 16-byte chunk k of row r lies at chunk k ^ (r & 7): the map's 128-byte swizzle
+                    // 16-byte chunk k of row r lies at chunk k ^ (r >> 1 & 3): the map's 64-byte swizzle
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         uint32_t w[4];
@@ -585,14 +588,14 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap mapM, const __grid_constant
                             const __nv_bfloat162 h = __floats2bfloat162_rn(f[8 * k + 2 * z], f[8 * k + 2 * z + 1]);
                             w[z] = *reinterpret_cast<const uint32_t*>(&h);
                         }
-                        const uint32_t at = buf + lane * 128 + (((4 * y + k) ^ (lane & 7)) << 4);
+                        const uint32_t at = buf + lane * 64 + ((k ^ (lane >> 1 & 3)) << 4);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
                                      ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
                     }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0 && j0 + c < p.whole) tma_store_2d(&mapO, buf, (int)(j0 + c), (int)row0);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0 && j0 + c0 < p.whole) tma_store_2d(&mapO, buf, (int)(j0 + c0), (int)row0);
             } else if (block == 32) {
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
@@ -816,17 +819,17 @@ int check_device(int* dev) {
     return *dev < 0 || *dev >= 64 ? GC_ERR_CUDA : GC_OK;
 }
 
-// Row-major bf16 output of whole 16 bytes, boxes of 32 rows x 128 bytes, 128-byte swizzle; what lies past the ends is
+// Row-major bf16 output of whole 16 bytes, boxes of 32 rows x 64 bytes, 64-byte swizzle; what lies past the ends is
 // not written.
 bool make_map_out(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t ld) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-    cuuint32_t box[2] = {64, 32};
+    cuuint32_t box[2] = {32, 32};
     cuuint32_t estr[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+              CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
            CUDA_SUCCESS;
 }
 
@@ -834,8 +837,8 @@ struct ImPlan { bool pair, staged; int bn; };
 
 // The tile that costs least by a count of cycles: rounds of tiles, each its products or loads, whichever is longer, or
 // its stores where they are longer still, and the stores of the last one.  The constants are fitted to 72 shapes with every
-// choice forced, one row to 60000 and contractions of 40 to 8192: 2.5 % behind the best choice on average, 20 % at
-// most.  bf16 outputs without staging would be 7 % behind (69 % at most), all of them staged 6 (60).
+// choice forced, one row to 60000 and contractions of 40 to 8192: 2 % behind the best choice on average, 10 % at
+// most.  bf16 outputs without staging would be 13 % behind (87 % at most), all of them staged 5 (49).
 ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, bool bf16) {
     ImPlan best{false, false, 16};
     double least = INFINITY;
@@ -985,7 +988,7 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
     // 64 x 50021 x 1000 15.8 / 14.1, 1 x 262144 x 1024 43.7 / 43.4; where more is written 48 x 131072 x 768 23.7 / 24.4,
     // 128 x 131072 x 768 29.6 / 32.1.
     p.once = !pl.staged && p.tiles_n == 1 && rows * cols * (bf16 ? 2 : 4) <= 20000000;
-    const size_t room = IM_SMEM - 1024 - IM_EPI * (IM_SCALES + (pl.staged ? 4096 : 0));
+    const size_t room = IM_SMEM - 1024 - IM_EPI * (IM_SCALES + (pl.staged ? 2048 : 0));
     p.stages = std::min(IM_MAX_ST, (int)(room / (CHUNK_BYTES + (size_t)n_rows * 128)));
     p.out = out; p.ldo = ldo; p.dev_status = dev_status;
     p.whole = cols & ~(int64_t)7;
