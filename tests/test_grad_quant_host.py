@@ -136,6 +136,11 @@ def test_lists_that_are_taken(binding):
     assert _passes(_clip(binding, {}, max_norm=0.0))
 
 
+def test_status_strings_of_lists(binding):
+    seen = {binding.status_string(i) for i in range(12)}
+    assert len(seen) == 12 and "unknown status" not in seen
+
+
 def test_workspace_of_a_list(binding):
     assert binding.gc_grad_workspace_bytes(-1) == 0
     assert binding.gc_grad_workspace_bytes((1 << 20) + 1) == 0
