@@ -157,6 +157,9 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError(f"Q/P must be float32 or bfloat16, got {t.dtype}")
 
 
+_CODES = {torch.float32: GC_F32, torch.bfloat16: GC_BF16}
+
+
 def gc_workspace_bytes(op: int, B: int, N: int, d: int, dtype: int) -> int:
     return int(_lib.gc_workspace_bytes(op, B, N, d, dtype))
 
@@ -449,14 +452,14 @@ def gc_dist_dot_block(Q, P, i0, bq, j0, bn, D_block) -> None:
         raise GradCacheError(rc, "gc_dist_dot_block")
 
 
-def _on_device(dev, *tensors):
-    """The library launches on the current device's current stream: refuses tensors that live elsewhere."""
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"tensors must be on one CUDA device, got one on {t.device}")
+def _on_device(dev, *others):
+    """The library launches on the current device's current stream: refuses tensors that live elsewhere (dev: a
+    tensor's device, -1 for the host; others: those of the other tensors)."""
+    for d in others:
+        if d != dev:
+            raise ValueError(f"tensors must be on one CUDA device, got devices {dev} and {d}")
     if dev < 0 or dev != _current_device():
         raise ValueError("tensors must be on the current CUDA device")
-    return dev
 
 
 def _scalar(t, dtype, name):
@@ -500,11 +503,11 @@ class GradList:
         self.n = len(self.grads)
         self.tensors = (_Tensor * max(self.n, 1))()
         self.address = ctypes.addressof(self.tensors)
-        self.device = self.grads[0].device if self.grads else None
+        self.device = self.grads[0].get_device() if self.grads else None
         for i, g in enumerate(self.grads):
             o = None if self.out is None else self.out[i]
             for t in (g, o):
-                if t is not None and (not t.is_cuda or t.device != self.device):
+                if t is not None and (not t.is_cuda or t.get_device() != self.device):
                     raise ValueError("gradients must be CUDA tensors of one device")
             code = _dtype_code(g)
             if o is not None and (o.dtype != g.dtype or o.shape != g.shape):
@@ -524,12 +527,15 @@ def gc_grad_workspace_bytes(n: int) -> int:
     return int(_lib.gc_grad_workspace_bytes(n))
 
 
-def _grad_args(grads, ws, *others):
+def _grad_args(grads, *others):
     """(GradList, current device): everything lives there."""
     if not isinstance(grads, GradList):
         grads = GradList(grads)
-    dev = _current_device() if grads.device is None else grads.device.index
-    return grads, _on_device(dev, ws, *others)
+    dev = grads.device
+    if dev is None:
+        dev = _current_device()
+    _on_device(dev, *[t.get_device() for t in others if t is not None])
+    return grads, dev
 
 
 def _grad_ws(grads, dev):
@@ -579,16 +585,18 @@ def gc_grad_clip(grads, max_norm, norm, sq_sum=None, ws=None, dev_status=None) -
 def gc_quantize_rows(X, q, scale) -> None:
     """scale[i] (float32) = max |X[i]| times 1/127 and q[i] (int8) = X[i] / scale[i] to the nearest integer."""
     shape, xs, qs = X.shape, X.stride(), q.stride()
-    if len(shape) != 2 or q.shape != shape or xs[1] != 1 or qs[1] != 1:
+    if len(xs) != 2 or q.shape != shape or xs[1] != 1 or qs[1] != 1:
         raise ValueError("X and q must be 2-D of one shape with unit stride along their rows")
     rows, d = shape
-    if q.dtype is not torch.int8 or scale.dtype is not torch.float32 or not scale.is_contiguous():
-        raise TypeError("q must be int8, scale contiguous float32")
+    code = _CODES.get(X.dtype)
+    if code is None or q.dtype is not torch.int8 or scale.dtype is not torch.float32 or not scale.is_contiguous():
+        raise TypeError("X must be float32 or bfloat16, q int8, scale contiguous float32")
     if scale.numel() != rows:
         raise ValueError("scale must hold one value for each row")
-    dev = _on_device(X.get_device(), q, scale)
-    rc = _lib.gc_quantize_rows(X.data_ptr(), xs[0], rows, d, _dtype_code(X), q.data_ptr(), qs[0],
-                               scale.data_ptr(), _raw_stream(dev))
+    dev = X.get_device()
+    _on_device(dev, q.get_device(), scale.get_device())
+    rc = _lib.gc_quantize_rows(X.data_ptr(), xs[0], rows, d, code, q.data_ptr(), qs[0], scale.data_ptr(),
+                               _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_quantize_rows")
 
@@ -603,14 +611,17 @@ def gc_matmul_i8(A, a_scale, B, b_scale, out, dev_status=None) -> None:
     cols, kb = B.shape
     if kb != k or out.shape != (rows, cols) or a_scale.numel() != rows or b_scale.numel() != cols:
         raise ValueError("shape mismatch")
-    if A.dtype is not torch.int8 or B.dtype is not torch.int8:
-        raise TypeError("A and B must be int8")
-    for s in (a_scale, b_scale):
-        if s.dtype is not torch.float32 or not s.is_contiguous():
-            raise TypeError("scales must be contiguous float32")
-    dev = _on_device(A.get_device(), a_scale, B, b_scale, out, dev_status)
+    code, i8, f32 = _CODES.get(out.dtype), torch.int8, torch.float32
+    if code is None or A.dtype is not i8 or B.dtype is not i8:
+        raise TypeError("A and B must be int8, out float32 or bfloat16")
+    if a_scale.dtype is not f32 or b_scale.dtype is not f32 or not a_scale.is_contiguous() \
+            or not b_scale.is_contiguous():
+        raise TypeError("scales must be contiguous float32")
+    dev = A.get_device()
+    _on_device(dev, a_scale.get_device(), B.get_device(), b_scale.get_device(), out.get_device(),
+               dev if dev_status is None else dev_status.get_device())
     rc = _lib.gc_matmul_i8(A.data_ptr(), sa[0], a_scale.data_ptr(), B.data_ptr(), sb[0], b_scale.data_ptr(), rows,
-                           cols, k, _dtype_code(out), out.data_ptr(), so[0], _ptr(dev_status), _raw_stream(dev))
+                           cols, k, code, out.data_ptr(), so[0], _ptr(dev_status), _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_matmul_i8")
 

@@ -328,6 +328,65 @@ def test_calls_that_overlap(binding):
         assert torch.equal(out, _product(*ops, F32))
 
 
+def test_different_calls_that_overlap(binding):
+    """Every kernel of these calls, and Steps 2 and 3, on streams of their own at the same time: each stream's results
+    are those of its calls alone."""
+    from paper_2101_06983_b200 import inputs
+
+    def products(rows, cols, k, dtype):
+        x = torch.randn(rows, k, device="cuda").to(dtype)
+        A, sa, B, sb = _operands(rows, cols, k, seed=rows)
+        out = torch.empty(rows, cols, dtype=dtype, device="cuda")
+
+        def step():
+            binding.gc_quantize_rows(x, A, sa)
+            binding.gc_matmul_i8(A, sa, B, sb, out)
+        return step, [A, sa, out]
+
+    def clipped(sizes):
+        g = [torch.randn(n, device="cuda") for n in sizes]
+        out = [torch.empty_like(t) for t in g]
+        lst, norm = binding.GradList(g, out), torch.empty(1, device="cuda")
+        ws = torch.empty(binding.gc_grad_workspace_bytes(len(g)), dtype=torch.uint8, device="cuda")
+        return lambda: binding.gc_grad_clip(lst, 0.5, norm, ws=ws), [norm, *out]
+
+    def trained():
+        prob = inputs.random_problem(700, 1400, 256, "bf16", seed=5, tau=0.5, scale=256 ** -0.5)
+        Q, P, pos = binding.problem_tensors(prob)
+        out = binding.Outputs(700, 1400, 256, binding.GC_BF16)
+        X, dW = torch.randn(700, 320, device="cuda").bfloat16(), torch.empty(256, 320, device="cuda")
+        ws = torch.empty(max(256, binding.gc_cache_apply_workspace_bytes(700, 256, 320)), dtype=torch.uint8, device="cuda")
+        lst, norm = binding.GradList([dW]), torch.empty(1, device="cuda")
+        ws2 = torch.empty(binding.gc_grad_workspace_bytes(1), dtype=torch.uint8, device="cuda")
+
+        def step():
+            binding.gc_build_cache(Q, P, pos, prob.tau, 0, out.loss, out.row_lse, out.dQ, out.dP, out.pos_logit, out.ws,
+                                   out.dev_status)
+            binding.gc_cache_apply(out.dQ, X, dW, False, ws=ws)
+            binding.gc_grad_clip(lst, 0.01, norm, ws=ws2)
+        return step, [out.loss, out.dQ, out.dP, dW, norm]
+
+    jobs = [products(1000, 3000, 768, F32), products(1, 500, 4096, F32), products(600, 2048, 1024, BF), products(30, 9000, 640, BF),
+            clipped([3000001]), clipped([1000, 20000, 5]), trained()]
+    want = []
+    for step, outs in jobs:
+        step()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in outs])
+        for t in outs:
+            t.zero_()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for _ in range(25):
+        for (step, _), s in zip(jobs, streams):
+            with torch.cuda.stream(s):
+                step()
+    torch.cuda.synchronize()
+    for (_, outs), w in zip(jobs, want):
+        for a, b in zip(outs, w):
+            assert torch.equal(a, b)
+
+
 def test_refusals_of_tensors(binding):
     A, sa, B, sb = _operands(16, 32, 64, seed=5)
     out = torch.empty(16, 32, device="cuda")
