@@ -215,6 +215,20 @@ def test_magnitudes(binding, dtype, size):
     assert abs(both.get_norm() - want) <= 2 * TOL_NORM * want
 
 
+def test_a_tensor_listed_twice(binding):
+    """The norm counts it twice; it is scaled into two outputs, but not where it lies."""
+    x = torch.randn(70001, device="cuda")
+    outs = [torch.empty_like(x) for _ in range(2)]
+    call = Call(binding, [x, x], outs)
+    sq = call.clip(3.0)
+    assert sq == call.get_norm() and abs(sq - 2 * _sum64([x])) <= 2 * TOL_NORM * sq
+    c = _factor(sq, 3.0)
+    assert all(torch.equal(o.cpu(), _scaled(x, c)) for o in outs)
+    with pytest.raises(binding.GradCacheError) as e:
+        binding.gc_grad_clip([x, x], 3.0, call.norm)
+    assert e.value.status == 10
+
+
 def test_bounds_at_the_ends(binding):
     x = torch.randn(3000, device="cuda")
     before = x.clone()
