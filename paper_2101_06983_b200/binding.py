@@ -479,8 +479,12 @@ def _dense(t) -> bool:
 
 def _as_matrix(t, like=None):
     """(rows, cols, pitch) of a tensor: one row where its values fill one stretch of memory (and those of
-    `like` lie in the same order), else a matrix with unit stride along its rows."""
-    if _dense(t) and (like is None or (_dense(like) and like.stride() == t.stride())):
+    `like`, a tensor of the same shape, lie in the same order), else a matrix with unit stride along its rows."""
+    if t.numel() == 0:
+        return 1, 0, 0
+    # (the stride of a dimension of size 1 says nothing)
+    if _dense(t) and (like is None or (_dense(like) and all(
+            a == b for a, b, size in zip(t.stride(), like.stride(), t.shape) if size > 1))):
         return 1, t.numel(), t.numel()
     if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
         return t.shape[0], t.shape[1], t.stride(0)

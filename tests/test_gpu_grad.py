@@ -174,6 +174,15 @@ def test_orders_of_dimensions(binding):
     assert torch.equal(a.cpu(), _scaled(before[0], c)) and torch.equal(b.cpu(), _scaled(before[1], c))
 
 
+def test_strides_of_single_places(binding):
+    """A 1 x 1 convolution's gradient of one memory format, its output of another: both lie alike."""
+    g = torch.randn(64, 3, 1, 1, device="cuda")
+    for src, like in ((g, g.as_strided(g.shape, (3, 1, 3, 3))), (g.as_strided(g.shape, (3, 1, 3, 3)), g)):
+        out = torch.empty_strided(like.shape, like.stride(), device="cuda")
+        call = Call(binding, [src], [out])
+        assert torch.equal(out.cpu(), _scaled(src, _factor(call.clip(0.5), 0.5)))
+
+
 @pytest.mark.parametrize("n", [31, 32, 33, 40, 95, 96, 97, 223, 224, 225, 539, 540, 541, 580, 1400])
 def test_lists_of_many_tensors(binding, n):
     """More tensors than one launch takes."""

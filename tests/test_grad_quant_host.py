@@ -177,6 +177,22 @@ def test_matrices_of_gradients(binding):
         f(z[0].t(), torch.zeros(4, 8))
 
 
+def test_strides_that_say_nothing(binding):
+    """A dimension of size 1 may have any stride, and a tensor without values any strides: 1 x 1 convolutions of one
+    memory format beside outputs of another, which lie alike."""
+    f = binding._as_matrix
+    conv = torch.zeros(64, 3, 1, 1)
+    last = conv.as_strided((64, 3, 1, 1), (3, 1, 3, 3))
+    assert f(conv, last) == f(last, conv) == (1, 192, 192)
+    one = torch.zeros(1, 5, 7)
+    odd = one.as_strided((1, 5, 7), (1, 7, 1))
+    assert f(one, odd) == f(odd, one) == (1, 35, 35)
+    with pytest.raises(ValueError):
+        f(torch.zeros(64, 3, 2, 1), torch.zeros(64, 2, 3, 1).permute(0, 2, 1, 3))      # these lie differently
+    assert f(torch.zeros(0, 4, 6)[:, :, ::2]) == (1, 0, 0)
+    assert f(torch.zeros(4, 0, 6)[:, :, ::2], torch.zeros(4, 0, 3)) == (1, 0, 0)
+
+
 def _quantize(binding, **over):
     a = dict(X=0x10000, ldx=64, rows=4, d=64, dtype=0, q=0x20000, ldq=64, scale=0x30000)
     a.update(over)
