@@ -338,8 +338,9 @@ int gc_dist_dot_block(const void* Q, int64_t ldq, const void* P, int64_t ldp, in
  *   gc_grad_clip    both: *norm = n, *sq_sum = n^2 (sq_sum may be NULL), out = c g.
  *
  * The two calls that write refuse a list in which a place that is written is read or written through another
- * tensor (GC_ERR_ALIAS): column ranges of one matrix that do not meet are no such places.  In place (`out`
- * NULL or equal to `data`, with the same pitch) nothing is written when c = 1.
+ * tensor, or through the tensor's own other place (GC_ERR_ALIAS): column ranges of one matrix that do not meet are no
+ * such places, matrices of different pitches count as if they were where their first and last bytes enclose one
+ * another's.  In place (`out` NULL or equal to `data`, with the same pitch) nothing is written when c = 1.
  * Squares are summed in fp32 over at most 64 values and in fp64 beyond, and in fp64 throughout where they
  * overflow or vanish in fp32: n is off by at most 2^-20 n for any finite values.  c is rounded to fp32,
  * then c g to the tensor's type.  Where n^2 is not finite (a NaN or an infinity among the gradients) *dev_status (may be NULL) gets

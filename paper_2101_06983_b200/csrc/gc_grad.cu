@@ -360,7 +360,13 @@ grad_cluster_kernel(const __grid_constant__ List<N> list, float max_norm, double
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-struct Span { uintptr_t lo, hi; int entry; bool written; };
+// The bytes from a tensor's first to its last, at one of its two places.
+struct Span {
+    uintptr_t lo, hi;
+    int64_t pitch;        // bytes from row to row; 0: one row
+    int64_t width;        // bytes of a row
+    bool written;
+};
 
 int elem_size(int dtype) { return dtype == GC_BF16 ? 2 : 4; }
 
@@ -388,19 +394,6 @@ int check_tensor(const gc_tensor& t, bool write, int64_t* count) {
 uintptr_t bytes_of(const gc_tensor& t, int64_t ld) {
     return (uintptr_t)(((t.rows - 1) * ld + t.cols) * elem_size(t.dtype));
 }
-// True where two spans that meet belong to column ranges of one matrix that do not.
-bool apart_by_columns(const gc_tensor& a, uintptr_t a_lo, int64_t a_ld, const gc_tensor& b, uintptr_t b_lo,
-                      int64_t b_ld) {
-    if (a.rows < 2 || b.rows < 2) {               // one row lies anywhere in the other's pitch
-        if (a.rows < 2) a_ld = b_ld; else b_ld = a_ld;
-        if (a.rows < 2 && b.rows < 2) return false;
-    }
-    const int64_t ea = elem_size(a.dtype), eb = elem_size(b.dtype);
-    if (a_ld * ea != b_ld * eb || a.cols > a_ld || b.cols > b_ld) return false;
-    const int64_t pitch = a_ld * ea, off = (int64_t)(b_lo - a_lo) % pitch;      // a_lo <= b_lo
-    return off >= a.cols * ea && off + b.cols * eb <= pitch;
-}
-
 // Spans that come in ascending order, in a few strands that lie apart (tensors of flat buffers, one for each type, and
 // their outputs): no two of them meet.  The usual list, told without sorting it.
 struct Strands {
@@ -426,6 +419,115 @@ struct Strands {
         return good;
     }
 };
+// How many of a set of intervals meet a given one: those that start before its end, less those that end before its start.
+// Counts lie in binary indexed trees over the ends that occur.
+class Intervals {
+public:
+    Intervals(const std::vector<int64_t>& starts, const std::vector<int64_t>& ends)
+        : starts_(starts), ends_(ends), n_starts_(starts.size() + 1), n_ends_(ends.size() + 1) {}
+    void add(int64_t a, int64_t b, int by) {
+        for (size_t i = below(starts_, a) + 1; i < n_starts_.size(); i += i & (~i + 1)) n_starts_[i] += by;
+        for (size_t i = below(ends_, b) + 1; i < n_ends_.size(); i += i & (~i + 1)) n_ends_[i] += by;
+    }
+    bool meet(int64_t a, int64_t b) const {
+        int64_t n = 0;
+        for (size_t i = below(starts_, b); i > 0; i &= i - 1) n += n_starts_[i];
+        for (size_t i = below(ends_, a + 1); i > 0; i &= i - 1) n -= n_ends_[i];
+        return n > 0;
+    }
+
+private:
+    static size_t below(const std::vector<int64_t>& v, int64_t x) { return std::lower_bound(v.begin(), v.end(), x) - v.begin(); }
+    const std::vector<int64_t>&starts_, &ends_;            // ascending, each value once
+    std::vector<int64_t> n_starts_, n_ends_;
+};
+
+// Goes through n spans in ascending order of their starts: drop(i) for those that end before the next starts, then
+// take(i), which is false where span i shares a place with one that has not been dropped.  False where any take is.
+template <typename Drop, typename Take>
+bool in_turn(const Span* s, size_t n, Drop drop, Take take) {
+    std::vector<size_t> by_end(n);
+    for (size_t i = 0; i < n; ++i) by_end[i] = i;
+    std::sort(by_end.begin(), by_end.end(), [&](size_t a, size_t b) { return s[a].hi < s[b].hi; });
+    size_t gone = 0;
+    for (size_t i = 0; i < n; ++i) {
+        for (; s[by_end[gone]].hi <= s[i].lo; ++gone) drop(by_end[gone]);     // (spans are not empty: i itself ends later)
+        if (!take(i)) return false;
+    }
+    return true;
+}
+
+// Whether rows of one pitch, and single rows among them, share no place that is written.  Where two spans meet, one starts
+// inside the other, and its first row shares a byte with the other's row there or the next exactly if the rows'
+// intervals modulo the pitch meet.
+bool rows_apart(const std::vector<Span>& s, int64_t pitch) {
+    struct Piece { int64_t a, b; };
+    std::vector<Piece> pieces(2 * s.size());               // the interval, and what of it passes the pitch's end
+    std::vector<int64_t> starts, ends;
+    for (size_t i = 0; i < s.size(); ++i) {
+        const int64_t a = (int64_t)(s[i].lo % (uintptr_t)pitch), b = a + std::min(s[i].width, pitch);
+        pieces[2 * i] = {a, std::min(b, pitch)};
+        pieces[2 * i + 1] = {0, std::max<int64_t>(0, b - pitch)};
+    }
+    for (const Piece& x : pieces) {
+        starts.push_back(x.a);
+        ends.push_back(x.b);
+    }
+    for (auto* v : {&starts, &ends}) {
+        std::sort(v->begin(), v->end());
+        v->erase(std::unique(v->begin(), v->end()), v->end());
+    }
+    Intervals all(starts, ends), written(starts, ends);
+    auto count = [&](size_t i, int by) {
+        for (size_t k = 2 * i; k < 2 * i + 2; ++k)
+            if (pieces[k].a < pieces[k].b) {
+                all.add(pieces[k].a, pieces[k].b, by);
+                if (s[i].written) written.add(pieces[k].a, pieces[k].b, by);
+            }
+    };
+    return in_turn(s.data(), s.size(), [&](size_t i) { count(i, -1); }, [&](size_t i) {
+        const Intervals& others = s[i].written ? all : written;
+        for (size_t k = 2 * i; k < 2 * i + 2; ++k)
+            if (pieces[k].a < pieces[k].b && others.meet(pieces[k].a, pieces[k].b)) return false;
+        count(i, 1);
+        return true;
+    });
+}
+// Whether n spans (ascending starts) share no place that is written.  Matrices of two pitches that meet count as if they did.
+bool spans_apart(const Span* s, size_t n) {
+    std::vector<int64_t> pitches;                          // 0, for single rows, among them
+    for (size_t i = 0; i < n; ++i) pitches.push_back(s[i].pitch);
+    std::sort(pitches.begin(), pitches.end());
+    pitches.erase(std::unique(pitches.begin(), pitches.end()), pitches.end());
+    struct Count { int64_t all = 0, written = 0; } rows;   // of matrices, whatever their pitch
+    std::vector<Count> of(pitches.size());
+    auto at = [&](size_t i) -> Count& {
+        return of[std::lower_bound(pitches.begin(), pitches.end(), s[i].pitch) - pitches.begin()];
+    };
+    auto count = [&](size_t i, int by) {
+        for (Count* c : {&at(i), s[i].pitch ? &rows : nullptr})
+            if (c) {
+                c->all += by;
+                c->written += s[i].written ? by : 0;
+            }
+    };
+    if (!in_turn(s, n, [&](size_t i) { count(i, -1); }, [&](size_t i) {
+            const Count& same = at(i);
+            const int64_t all = s[i].pitch ? rows.all - same.all : same.all;
+            const int64_t written = s[i].pitch ? rows.written - same.written : same.written;
+            count(i, 1);
+            return (s[i].written ? all : written) == 0;
+        }))
+        return false;
+    for (const int64_t pitch : pitches)
+        if (pitch) {
+            std::vector<Span> some;
+            for (size_t i = 0; i < n; ++i)
+                if (s[i].pitch == 0 || s[i].pitch == pitch) some.push_back(s[i]);
+            if (!rows_apart(some, pitch)) return false;
+        }
+    return true;
+}
 // No place that is written may be read or written through another tensor of the list.
 int check_overlap(const gc_tensor* list, int64_t n) {
     Strands strands;
@@ -448,24 +550,22 @@ int check_overlap(const gc_tensor* list, int64_t n) {
     for (int64_t i = 0; i < n; ++i)
         if (list[i].rows > 0 && list[i].cols > 0) {
             const gc_tensor& t = list[i];
-            const uintptr_t lo = (uintptr_t)t.data, out = (uintptr_t)t.out;
             const bool in_place = !t.out || t.out == t.data;
-            s.push_back({lo, lo + bytes_of(t, t.ld), (int)i, in_place});
-            if (!in_place) s.push_back({out, out + bytes_of(t, t.ld_out), (int)i, true});
+            auto add = [&](const void* p, int64_t ld, bool written) {
+                const uintptr_t lo = (uintptr_t)p;
+                const int64_t es = elem_size(t.dtype);
+                s.push_back({lo, lo + bytes_of(t, ld), t.rows > 1 ? ld * es : 0, t.cols * es, written});
+            };
+            add(t.data, t.ld, in_place);
+            if (!in_place) add(t.out, t.ld_out, true);
         }
     std::sort(s.begin(), s.end(), [](const Span& a, const Span& b) { return a.lo < b.lo; });
-    auto pitch = [&](const Span& x) {
-        const gc_tensor& t = list[x.entry];
-        return x.lo == (uintptr_t)t.data ? t.ld : t.ld_out;
-    };
-    int64_t pairs = 0;
-    for (size_t i = 0; i < s.size(); ++i)
-        for (size_t j = i + 1; j < s.size() && s[j].lo < s[i].hi; ++j) {
-            if (++pairs > (int64_t)1 << 24) return GC_ERR_LIMIT;
-            if ((s[i].written || s[j].written) &&
-                !apart_by_columns(list[s[i].entry], s[i].lo, pitch(s[i]), list[s[j].entry], s[j].lo, pitch(s[j])))
-                return GC_ERR_ALIAS;
-        }
+    // stretches of spans that meet, one after the other
+    for (size_t i = 0, j; i < s.size(); i = j) {
+        uintptr_t end = s[i].hi;
+        for (j = i + 1; j < s.size() && s[j].lo < end; ++j) end = std::max(end, s[j].hi);
+        if (j - i > 1 && !spans_apart(s.data() + i, j - i)) return GC_ERR_ALIAS;
+    }
     return GC_OK;
 }
 

@@ -121,6 +121,75 @@ def test_shared_places_in_long_lists(binding, n, gap):
         assert _clip(binding, *[dict(t, out=None) for t in twice]) == ALIAS
 
 
+def _bytes(t, where):
+    es, ld = (2 if t["dtype"] else 4), t["ld" if where == "data" else "ld_out"]
+    rows = range(t["rows"])
+    return t[where], [range(t[where] + i * ld * es, t[where] + i * ld * es + t["cols"] * es) for i in rows], \
+        ld * es if t["rows"] > 1 else 0
+
+
+def _shares(tensors):
+    """Whether a byte that is written belongs to another tensor, or to a matrix of another pitch that reaches
+    across it: every byte looked at."""
+    spans = []
+    for t in tensors:
+        spans.append((*_bytes(t, "data")[1:], t["out"] is None))
+        if t["out"] is not None:
+            spans.append((*_bytes(t, "out")[1:], True))
+    sets = [{b for r in rows for b in r} for rows, _, _ in spans]
+    for i, (a, pa, wa) in enumerate(spans):
+        for k, (b, pb, wb) in enumerate(spans[:i]):
+            if (wa or wb) and (sets[i] & sets[k] or pa and pb and pa != pb and a[0][0] < b[-1][-1] + 1
+                               and b[0][0] < a[-1][-1] + 1):
+                return True
+    return False
+
+
+@needs_no_gpu
+def test_shared_places_byte_by_byte(binding):
+    """Small lists of rows, matrices of a few pitches and both types, packed closely enough to meet."""
+    import random
+    rng = random.Random(3)
+    seen = [0, 0]
+    for turn in range(6000):
+        tensors, pitch = [], rng.choice([8, 12, 24])
+        for _ in range(rng.randint(2, 6)):
+            dtype, rows = rng.randint(0, 1), rng.choice([1, 1, 2, 3, 5])
+            es = 2 if dtype else 4
+            p = pitch if rng.random() < 0.9 else 16
+            cols = rng.randint(1, max(1, p // es // rng.choice([1, 2, 3])))
+            if rows == 1 and rng.random() < 0.2:
+                cols = rng.randint(1, 20)
+            place = lambda: 0x1000 + 4 * rng.randint(0, 60 if turn % 2 else 25)  # noqa: E731
+            tensors.append(dict(data=place(), out=None if rng.random() < 0.7 else place() + 0x200 * rng.randint(0, 1),
+                                rows=rows, cols=cols, ld=p // es, ld_out=p // es, dtype=dtype))
+            if tensors[-1]["out"] == tensors[-1]["data"]:
+                tensors[-1]["out"] = None
+        want = _shares(tensors)
+        seen[want] += 1
+        got = _clip(binding, *tensors)
+        assert got == ALIAS if want else _passes(got), tensors
+    assert min(seen) > 500
+
+
+@needs_no_gpu
+def test_many_column_ranges_of_one_matrix(binding):
+    """A matrix cut into more column ranges than can be compared two by two; then one of them moved by an element, or
+    scaled into another."""
+    n, width = 9000, 3
+    ranges = [dict(data=0x100000 + 4 * width * i, rows=5, cols=width, ld=n * width) for i in range(n)]
+    assert _passes(_clip(binding, *ranges))
+    # ranges in no order, and of the upper and the lower half of the rows
+    ranges = [dict(r, rows=3) for r in ranges] + [dict(r, rows=2, data=r["data"] + 4 * 3 * n * width) for r in ranges]
+    assert _passes(_clip(binding, *ranges[::-1]))
+    for k in (0, n // 3, n + 17, 2 * n - 2):
+        bad = [dict(r) for r in ranges]
+        bad[k]["data"] += 4
+        assert _clip(binding, *bad) == ALIAS
+        bad[k].update(data=ranges[k]["data"], out=ranges[k + 1]["data"], ld_out=n * width)
+        assert _clip(binding, *bad) == ALIAS
+
+
 @needs_no_gpu
 def test_lists_that_are_taken(binding):
     assert _passes(_clip(binding))
