@@ -329,7 +329,8 @@ int gc_dist_dot_block(const void* Q, int64_t ldq, const void* P, int64_t ldp, in
  * A list is a HOST array of n_tensors gc_tensor (read during the call only), each a matrix of GC_F32 or
  * GC_BF16 values in device memory; a list may mix both.  Tensors may be empty, of any length, and start on
  * any multiple of their element size; vectors of 16 bytes are used where start and pitch allow.  n_tensors
- * may be 0 (norm 0) and at most 2^20; a tensor of several rows has at most 2^31 columns (else GC_ERR_LIMIT).
+ * may be 0 (norm 0) and at most 2^20; a tensor of several rows has at most 2^31 columns, a list at most 2^42 elements
+ * (else GC_ERR_LIMIT).
  *
  *   gc_grad_norm    *sq_sum = n^2 (double), *norm = n (float); either may be NULL.  No tensor is written
  *                   (`out` and `ld_out` are not read) and one may be listed twice: it counts twice.

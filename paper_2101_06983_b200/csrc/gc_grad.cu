@@ -33,6 +33,9 @@ constexpr int GR_CLUSTER = 16;
 constexpr uint32_t GR_SHORT = 16;
 constexpr int GR_SLOTS = 1024;                 // partial sums of a launch
 constexpr double GR_EPS = 1e-6;
+// Elements of a list: its tiles, of 2^11 single elements at least but for one of each tensor, and the strides that kernels
+// add to their indices stay below 2^32.
+constexpr int64_t GR_MOST = (int64_t)1 << 42;
 
 enum EntryMode : uint32_t { FLAT_VEC = 0, ROWS_VEC = 1, ELEM = 2 };
 
@@ -615,24 +618,20 @@ int current_device() {
 
 int64_t groups_of(int64_t n) { return std::max<int64_t>(1, (n + MANY - 1) / MANY); }
 
-// The next group of at most MANY tensors, from tensor *i on.
-int next_group(const gc_tensor* list, int64_t n, bool write, int64_t* i, List<MANY>& l) {
+// The next group, of MANY tensors that are not empty or what is left of them, from tensor *i on: no list has more groups than
+// groups_of its length, for which the workspace has room.
+void next_group(const gc_tensor* list, int64_t n, bool write, int64_t* i, List<MANY>& l) {
     l.n = 0;
-    int64_t tiles = 0;
+    int64_t tiles = 0;                                 // (GR_MOST bounds them)
     for (; *i < n && l.n < MANY; ++*i) {
         if (list[*i].rows == 0 || list[*i].cols == 0) continue;
         int64_t more = 0;
         Entry e = entry_for(list[*i], write, &more);
-        if (tiles + more > (int64_t)UINT32_MAX) {
-            if (l.n == 0) return GC_ERR_LIMIT;
-            break;
-        }
         l.first[l.n] = (uint32_t)tiles;
         tiles += more;
         l.e[l.n++] = e;
     }
     l.tiles = (uint32_t)tiles;
-    return GC_OK;
 }
 // go(list) with the smallest list type that holds the group.
 template <int N, typename Go>
@@ -662,11 +661,14 @@ int check_list(const gc_tensor* list, int64_t n, bool write) {
     if (n < 0) return GC_ERR_SHAPE;
     if (n > 0 && !list) return GC_ERR_NULL;
     if (n > (int64_t)1 << 20) return GC_ERR_LIMIT;
+    int64_t all = 0;
     for (int64_t i = 0; i < n; ++i) {
         int64_t count;
         const int rc = check_tensor(list[i], write, &count);
         if (rc) return rc;
+        all += count;                                  // (at most 2^20 times 2^40)
     }
+    if (all > GR_MOST) return GC_ERR_LIMIT;
     return write ? check_overlap(list, n) : GC_OK;
 }
 int check_ws(const void* ws, size_t ws_bytes, int64_t n) {
@@ -727,8 +729,9 @@ int scale_all(const gc_tensor* list, int64_t n, const double* part, int slots, f
     int64_t i = 0;
     bool tell = true;
     do {
-        int rc = next_group(list, n, true, &i, group);
-        if (rc || (rc = launch_scale(group, part, slots, max_norm, sq_sum, norm, dev_status, tell, st))) return rc;
+        next_group(list, n, true, &i, group);
+        const int rc = launch_scale(group, part, slots, max_norm, sq_sum, norm, dev_status, tell, st);
+        if (rc) return rc;
         tell = false;
     } while (i < n);
     return GC_OK;
@@ -756,11 +759,13 @@ int gc_grad_norm(const gc_tensor* list, int64_t n, double* sq_sum, float* norm, 
     List<MANY> group;
     int64_t i = 0;
     int slots = 0;
-    if ((rc = next_group(list, n, false, &i, group))) return rc;
+    next_group(list, n, false, &i, group);
     if (i >= n && is_short(group)) return launch_short<false>(group, 0.f, sq_sum, norm, dev_status, st);
     if ((rc = launch_squares(group, part, &slots, st))) return rc;
-    while (i < n)
-        if ((rc = next_group(list, n, false, &i, group)) || (rc = launch_squares(group, part, &slots, st))) return rc;
+    while (i < n) {
+        next_group(list, n, false, &i, group);
+        if ((rc = launch_squares(group, part, &slots, st))) return rc;
+    }
     if (launch_chained(grad_norm_kernel, dim3(1), GR_THREADS, 0, 1, st, part, slots, sq_sum, norm, dev_status) !=
         cudaSuccess) {
         cudaGetLastError();
@@ -794,13 +799,15 @@ int gc_grad_clip(const gc_tensor* list, int64_t n, float max_norm, double* sq_su
     List<MANY> group;
     int64_t i = 0;
     int slots = 0;
-    if ((rc = next_group(list, n, true, &i, group))) return rc;
+    next_group(list, n, true, &i, group);
     if (i >= n && is_short(group)) return launch_short<true>(group, max_norm, sq_sum, norm, dev_status, st);
     if ((rc = launch_squares(group, part, &slots, st))) return rc;
     if (i >= n)                                        // the only group: its list serves both passes
         return launch_scale(group, part, slots, max_norm, sq_sum, norm, dev_status, true, st);
-    while (i < n)
-        if ((rc = next_group(list, n, true, &i, group)) || (rc = launch_squares(group, part, &slots, st))) return rc;
+    while (i < n) {
+        next_group(list, n, true, &i, group);
+        if ((rc = launch_squares(group, part, &slots, st))) return rc;
+    }
     return scale_all(list, n, part, slots, max_norm, sq_sum, norm, dev_status, st);
 } catch (...) {
     return GC_ERR_HOST;

@@ -70,6 +70,19 @@ def test_lists_that_are_refused(binding):
     assert _clip(binding, {}, wsb=64) == WORKSPACE
 
 
+def test_lists_of_too_many_values(binding):
+    """A tensor may be listed any number of times for its norm, but a list has an end: its tiles are counted in 32 bits, and
+    the workspace holds the partial sums of one launch for each 540 tensors."""
+    big = dict(rows=1 << 20, cols=(1 << 17) - 1, ld=1 << 17, dtype=1)            # single elements, 2^26 tiles
+    assert _norm(binding, *[big] * 540) == LIMIT
+    assert _norm(binding, *[big] * 33) == LIMIT
+    assert _norm(binding, *[dict(rows=1, cols=1 << 40)] * 4, {}) == LIMIT
+    assert _clip(binding, *[dict(big, data=(k + 1) << 48) for k in range(33)]) == LIMIT
+    if not torch.cuda.is_available():
+        assert _passes(_norm(binding, *[big] * 32))
+        assert _passes(_norm(binding, *[dict(rows=1, cols=1 << 40)] * 4))
+
+
 def test_places_that_two_tensors_share(binding):
     assert _clip(binding, {}, {}) == ALIAS                          # the same tensor twice
     assert _clip(binding, {}, dict(data=0x10000 + 4 * 255)) == ALIAS
