@@ -551,6 +551,7 @@ def gc_grad_norm(grads, norm=None, sq_sum=None, ws=None, dev_status=None) -> Non
     (float64) its square; either may be left out.  A NaN or an infinity sets GC_DEV_GRAD_NONFINITE."""
     _scalar(norm, torch.float32, "norm")
     _scalar(sq_sum, torch.float64, "sq_sum")
+    _scalar(dev_status, torch.int32, "dev_status")
     grads, dev = _grad_args(grads, ws, norm, sq_sum, dev_status)
     if ws is None:
         ws = _grad_ws(grads, dev)
@@ -564,6 +565,7 @@ def gc_grad_scale(grads, sq_sum, max_norm, dev_status=None) -> None:
     """Scales the gradients (in place, or into the list's `out`) by min(1, max_norm / (n + 1e-6)), with n^2 =
     sq_sum[0] (float64): of gc_grad_norm, or summed over ranks that hold different gradients."""
     _scalar(sq_sum, torch.float64, "sq_sum")
+    _scalar(dev_status, torch.int32, "dev_status")
     grads, dev = _grad_args(grads, None, sq_sum, dev_status)
     rc = _lib.gc_grad_scale(grads.address, grads.n, _ptr(sq_sum), max_norm, _ptr(dev_status),
                             _raw_stream(dev))
@@ -577,6 +579,7 @@ def gc_grad_clip(grads, max_norm, norm, sq_sum=None, ws=None, dev_status=None) -
     finite."""
     _scalar(norm, torch.float32, "norm")
     _scalar(sq_sum, torch.float64, "sq_sum")
+    _scalar(dev_status, torch.int32, "dev_status")
     grads, dev = _grad_args(grads, ws, norm, sq_sum, dev_status)
     if ws is None:
         ws = _grad_ws(grads, dev)
@@ -621,6 +624,7 @@ def gc_matmul_i8(A, a_scale, B, b_scale, out, dev_status=None) -> None:
     if a_scale.dtype is not f32 or b_scale.dtype is not f32 or not a_scale.is_contiguous() \
             or not b_scale.is_contiguous():
         raise TypeError("scales must be contiguous float32")
+    _scalar(dev_status, torch.int32, "dev_status")
     dev = A.get_device()
     _on_device(dev, a_scale.get_device(), B.get_device(), b_scale.get_device(), out.get_device(),
                dev if dev_status is None else dev_status.get_device())

@@ -240,6 +240,20 @@ def test_lists_of_host_tensors_are_refused(binding):
         binding.gc_quantize_rows(torch.zeros(2, 16), torch.zeros(2, 16, dtype=torch.int8), torch.zeros(2))
 
 
+def test_status_words_of_other_types_are_refused(binding):
+    """Kernels set bits of a 32-bit word there."""
+    norm, sq, f = torch.zeros(1), torch.zeros(1, dtype=torch.float64), torch.zeros(1, 16)
+    q, s = torch.zeros(1, 16, dtype=torch.int8), torch.zeros(1)
+    for bad in (torch.zeros(1, dtype=torch.uint8), torch.zeros(1), torch.zeros(1, dtype=torch.int64),
+                torch.zeros(0, dtype=torch.int32)):
+        for call in (lambda: binding.gc_grad_norm([f], norm, dev_status=bad),
+                     lambda: binding.gc_grad_scale([f], sq, 1.0, dev_status=bad),
+                     lambda: binding.gc_grad_clip([f], 1.0, norm, dev_status=bad),
+                     lambda: binding.gc_matmul_i8(q, s, q, s, torch.zeros(1, 1), dev_status=bad)):
+            with pytest.raises(TypeError):
+                call()
+
+
 def test_matrices_of_gradients(binding):
     """How tensors are described: one row where they are dense, whatever the order of their dimensions."""
     z = torch.zeros(6, 8, 4)
