@@ -227,6 +227,8 @@ def clip_over_ranks(grads, max_norm, sq_sum, ws=None, dev_status=None, kernels=N
     and sets GC_DEV_GRAD_NONFINITE in everyone's dev_status.  Gradients that are the same on all ranks (an
     all-reduce of dW) need no exchange: binding.gc_grad_clip."""
     kernels = kernels or LibraryKernels()
+    if hasattr(grads, "__next__"):                     # both passes go through them
+        grads = list(grads)
     kernels.grad_sq_sum(grads, sq_sum, ws, dev_status)
     if _world(group)[0] > 1:
         dist.all_reduce(sq_sum, op=dist.ReduceOp.SUM, group=group)

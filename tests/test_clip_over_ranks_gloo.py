@@ -74,3 +74,13 @@ def test_one_rank_needs_no_group():
     sharded.clip_over_ranks(grads, 1.0, sq, dev_status=torch.zeros(1, dtype=torch.int32), kernels=PlainKernels())
     assert sq.item() == 16.0
     torch.testing.assert_close(grads[0], torch.full((4,), 0.5), rtol=1e-6, atol=0)
+
+
+def test_gradients_that_can_be_gone_through_once():
+    """(p.grad for p in parameters): read by both passes."""
+    from paper_2101_06983_b200 import sharded
+    grads, sq = [torch.full((4,), 2.0), torch.full((2, 3), -1.0)], torch.zeros(1, dtype=torch.float64)
+    sharded.clip_over_ranks((g for g in grads), 1.0, sq, dev_status=torch.zeros(1, dtype=torch.int32), kernels=PlainKernels())
+    assert sq.item() == 22.0
+    for g, v in zip(grads, (2.0, -1.0)):
+        torch.testing.assert_close(g, torch.full_like(g, v / math.sqrt(22.0)), rtol=1e-6, atol=0)
