@@ -26,11 +26,12 @@ constexpr int GR_PER = 4;                      // of a thread, all under way at 
 // 180 / 89 / 334, 3 and 2 177 / 88 / 332, 4 and 3 180 / 89 / 336; tiles of 16 KB 188 / 95 / 370, of 64 KB 179 / 90 / 332.
 constexpr int GR_B1 = 3, GR_B2 = 2;
 constexpr int GR_TILE_UNITS = GR_THREADS * GR_PER;   // 16-byte vectors of a tile; single elements where they do not fit
-constexpr int GR_CLUSTER = 16;
 // Lists of at most so many tiles take one launch of a cluster instead of two of the whole device.  Measured, us a call back to
 // back from the host, then in a graph, 8 tiles: norm 5.0 and 3.4 (two launches 7.0 and 3.2), clipping 5.3 and 5.4 (7.0
 // and 4.6); 16 tiles: clipping 5.5 and 5.5 (7.1 and 4.8); 36: 7.8 and 7.7 (7.1 and 4.9).
 constexpr uint32_t GR_SHORT = 16;
+constexpr int GR_CLUSTER = 8;                  // two tiles to a CTA
+static_assert(2 * GR_CLUSTER >= GR_SHORT, "the largest cluster takes the longest short list in a round");
 constexpr int GR_SLOTS = 1024;                 // partial sums of a launch
 constexpr double GR_EPS = 1e-6;
 // Elements of a list: its tiles, of 2^11 single elements at least but for one of each tensor, and the strides that kernels
@@ -699,20 +700,6 @@ int launch_scale(const List<MANY>& group, const double* part, int slots, float m
 bool is_short(const List<MANY>& group) { return group.tiles <= GR_SHORT && group.n <= FEW; }
 template <bool CLIP>
 int launch_short(const List<MANY>& group, float max_norm, double* sq_sum, float* norm, int* dev_status, cudaStream_t st) {
-    int dev = 0;
-    static bool configured_on[64] = {false};             // the attribute belongs to (kernel, device)
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
-        cudaGetLastError();
-        return GC_ERR_CUDA;
-    }
-    if (!configured_on[dev]) {
-        if (cudaFuncSetAttribute(grad_cluster_kernel<FEW, CLIP>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
-            cudaSuccess) {
-            cudaGetLastError();
-            return GC_ERR_CUDA;
-        }
-        configured_on[dev] = true;
-    }
     int ctas = 1;
     while (ctas < GR_CLUSTER && 2u * ctas < group.tiles) ctas *= 2;
     const cudaError_t e = with_size<FEW>(group, [&](const List<FEW>& l) {
