@@ -386,6 +386,9 @@ int gc_grad_clip(const gc_tensor* tensors, int64_t n_tensors, float max_norm, do
  * is not read).  At most 2^30 rows and columns (else GC_ERR_LIMIT).  A and B may be the same buffer.  Asynchronous on cuda_stream, deterministic; no workspace.
  * GC_DEV_WAIT_LIMIT in *dev_status (may be NULL) as for the other calls.
  */
+/* How gc_matmul_i8 covers a product: "tcgen05" (a CTA to a tile), "tcgen05-pairs" (two CTAs), the same with "-staged" (bf16
+ * outputs through shared memory), "tcgen05-split" (clusters share the contraction), or "invalid". */
+const char* gc_matmul_i8_plan_name(int64_t rows, int64_t cols, int64_t k, int out_dtype);
 int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dtype, int8_t* q, int64_t ldq,
                      float* scale, void* cuda_stream);
 int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb,

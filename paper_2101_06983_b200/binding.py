@@ -29,7 +29,7 @@ EXPORTS = ("gc_workspace_bytes", "gc_plan_name", "gc_kernel_launches", "gc_loss_
            "gc_multi_pos_workspace_bytes", "gc_build_cache_multi_pos",
            "gc_two_direction_workspace_bytes", "gc_build_cache_two_direction",
            "gc_grad_workspace_bytes", "gc_grad_norm", "gc_grad_scale", "gc_grad_clip",
-           "gc_quantize_rows", "gc_matmul_i8")
+           "gc_quantize_rows", "gc_matmul_i8", "gc_matmul_i8_plan_name")
 GC_STATIC_SCRATCH_BYTES = 2 << 20
 
 
@@ -129,6 +129,8 @@ def _load() -> ctypes.CDLL:
     lib.gc_quantize_rows.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
     lib.gc_matmul_i8.restype = i32
     lib.gc_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, i64, i64, i64, i32, vp, i64, vp, vp]
+    lib.gc_matmul_i8_plan_name.restype = ctypes.c_char_p
+    lib.gc_matmul_i8_plan_name.argtypes = [i64, i64, i64, i32]
     lib.gc_selftest_wait_limit.restype = i32
     lib.gc_selftest_wait_limit.argtypes = [ctypes.c_uint64, vp, vp, vp]
     lib.gc_profile_enable.restype = i32
@@ -606,6 +608,10 @@ def gc_quantize_rows(X, q, scale) -> None:
                                _raw_stream(dev))
     if rc != 0:
         raise GradCacheError(rc, "gc_quantize_rows")
+
+
+def gc_matmul_i8_plan_name(rows: int, cols: int, k: int, out_dtype: int) -> str:
+    return _lib.gc_matmul_i8_plan_name(rows, cols, k, out_dtype).decode()
 
 
 def gc_matmul_i8(A, a_scale, B, b_scale, out, dev_status=None) -> None:

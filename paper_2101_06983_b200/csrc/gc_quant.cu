@@ -212,6 +212,7 @@ quantize_rows_kernel(const void* X, int64_t ldx, int64_t rows, int64_t d, int8_t
 // ---------------------------------------------------------------------------------------------------
 // Product
 // ---------------------------------------------------------------------------------------------------
+constexpr int64_t IM_MAX_K = 131071;       // so many products of -128 and -128 fit 31 bits
 constexpr int IM_KB = 128;                 // contraction depth of a ring stage: one swizzle row of bytes
 constexpr int IM_MAX_ST = 11;
 constexpr size_t IM_SMEM = 225 * 1024;
@@ -956,6 +957,17 @@ int gc_quantize_rows(const void* X, int64_t ldx, int64_t rows, int64_t d, int dt
     return GC_OK;
 }
 
+const char* gc_matmul_i8_plan_name(int64_t rows, int64_t cols, int64_t k, int out_dtype) {
+    const int64_t most = (int64_t)1 << 30;
+    if ((out_dtype != GC_F32 && out_dtype != GC_BF16) || rows <= 0 || cols <= 0 || k <= 0 || rows > most || cols > most ||
+        k > IM_MAX_K)
+        return "invalid";
+    if (split_ctas(rows, cols, k) > 1) return "tcgen05-split";
+    const ImPlan pl = make_im_plan(rows, cols, k, out_dtype == GC_BF16);
+    if (pl.staged) return pl.pair ? "tcgen05-pairs-staged" : "tcgen05-staged";
+    return pl.pair ? "tcgen05-pairs" : "tcgen05";
+}
+
 int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb,
                  const float* b_scale, int64_t rows, int64_t cols, int64_t k, int out_dtype, void* out, int64_t ldo,
                  int* dev_status, void* cuda_stream) {
@@ -965,7 +977,7 @@ int gc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_
         (rc = check_matrix(out, rows, cols, &ldo, out_dtype == GC_BF16 ? 2 : 4)))
         return rc;
     if (!a_scale || !b_scale) return GC_ERR_NULL;
-    if (k > 131071) return GC_ERR_LIMIT;           // 2^14 (k of -128 times -128) must fit 31 bits
+    if (k > IM_MAX_K) return GC_ERR_LIMIT;
     int dev;
     if ((rc = check_device(&dev))) return rc;
     const bool bf16 = out_dtype == GC_BF16;

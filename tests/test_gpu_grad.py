@@ -165,6 +165,26 @@ def test_column_ranges_of_one_matrix(binding):
     assert torch.equal(big.cpu(), expect)
 
 
+def test_many_column_ranges_of_one_matrix(binding):
+    """More ranges than can be compared two by two, and rows of the other type between them."""
+    n = 7000
+    big = torch.randn(3, 4 * n, device="cuda")
+    gap = big[1, 7:9].view(BF)                                  # of which a range leaves the first two free
+    gap.copy_(torch.tensor([1.5, -2.0, 1.0, 1.0]))
+    before = big.clone()
+    ranges = [big[:, 4 * i:4 * i + 3] for i in range(1, n)] + [gap[:2]]
+    call = Call(binding, ranges)
+    want = _sum64(ranges)
+    sq = call.clip(1.0)
+    assert abs(sq - want) <= 2 * TOL_NORM * want
+    expect = before.cpu()
+    c = _factor(sq, 1.0)
+    for k in range(3):
+        expect[:, 4 + k::4] = _scaled(before, c)[:, 4 + k::4]
+    expect.view(BF)[1, 14:16] = _scaled(before.view(BF)[1, 14:16], c)
+    assert torch.equal(big.cpu().view(torch.int32), expect.view(torch.int32))
+
+
 def test_orders_of_dimensions(binding):
     a = torch.randn(12, 7, 5, 3, device="cuda").to(memory_format=torch.channels_last)
     b = torch.randn(40, 30, device="cuda").t()

@@ -196,6 +196,28 @@ def test_products(binding, rows, cols, k, dtype):
     _check_product(binding, A, sa, B, sb, dtype, pad=cols % 2)
 
 
+# Where every CTA (or pair) has three tiles and more, however large they are: accumulators, staging buffers and the places of
+# the scales are used again.  Odd widths and counts, short and long contractions, for each form with bf16 outputs.
+LONG_RUNS = [
+    ("tcgen05-pairs-staged", 4100, 8197, 768), ("tcgen05-pairs-staged", 3001, 20011, 300),
+    ("tcgen05-pairs", 16390, 771, 4096), ("tcgen05-pairs", 20, 60001, 5978), ("tcgen05-pairs", 70, 60001, 1500),
+    ("tcgen05-staged", 2500, 9001, 90), ("tcgen05-staged", 19315, 1363, 65), ("tcgen05-staged", 151, 60003, 23),
+    ("tcgen05", 16, 60001, 16), ("tcgen05", 9, 70005, 100),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("plan,rows,cols,k", LONG_RUNS)
+def test_products_of_many_tiles(binding, plan, rows, cols, k, dtype):
+    if dtype is BF:
+        assert binding.gc_matmul_i8_plan_name(rows, cols, k, binding.GC_BF16) == plan
+        m, n = (rows, cols) if "staged" in plan else (cols, rows)
+        m_rows, units = (256, 74) if "pairs" in plan else (128, 148)
+        assert -(-m // m_rows) * -(-n // 256) > 3 * units
+    A, sa, B, sb = _operands(rows, cols, k, seed=rows + k, pad=k % 2)
+    _check_product(binding, A, sa, B, sb, dtype, pad=cols % 3)
+
+
 @pytest.mark.parametrize("rows", [1, 40, 700])
 def test_the_longest_contraction(binding, rows):
     """-128 times -128 over the longest rows: the sum still fits 31 bits."""

@@ -321,3 +321,15 @@ def test_8_bit_calls_that_are_refused(binding):
         assert _matmul(binding, **bad) == ALIGN
     assert _matmul(binding, k=131072, lda=131072, ldb=131072) == LIMIT
     assert _matmul(binding, cols=(1 << 30) + 1, ldo=(1 << 30) + 4) == LIMIT
+
+
+def test_names_of_product_plans(binding):
+    """Each form of the product is chosen for some sizes (148 SMs)."""
+    name = binding.gc_matmul_i8_plan_name
+    assert name(1, 768, 4096, binding.GC_F32) == name(1, 768, 4096, binding.GC_BF16) == "tcgen05-split"
+    assert name(4100, 8197, 768, binding.GC_BF16) == "tcgen05-pairs-staged"
+    assert name(4100, 8197, 768, binding.GC_F32) == name(16390, 771, 4096, binding.GC_BF16) == "tcgen05-pairs"
+    assert name(2500, 9001, 90, binding.GC_BF16) == "tcgen05-staged"
+    assert name(2500, 9001, 90, binding.GC_F32) == name(16, 60001, 16, binding.GC_BF16) == "tcgen05"
+    for bad in ((0, 1, 1, 0), (1, 0, 1, 0), (1, 1, 0, 0), (1, 1, 131072, 0), (1, 1, 1, 2), ((1 << 30) + 1, 1, 1, 0)):
+        assert name(*bad) == "invalid"
