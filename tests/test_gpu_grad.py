@@ -200,7 +200,8 @@ def test_strides_of_single_places(binding):
     for src, like in ((g, g.as_strided(g.shape, (3, 1, 3, 3))), (g.as_strided(g.shape, (3, 1, 3, 3)), g)):
         out = torch.empty_strided(like.shape, like.stride(), device="cuda")
         call = Call(binding, [src], [out])
-        assert torch.equal(out.cpu(), _scaled(src, _factor(call.clip(0.5), 0.5)))
+        c = _factor(call.clip(0.5), 0.5)
+        assert torch.equal(out.cpu(), _scaled(src, c))
 
 
 @pytest.mark.parametrize("n", [31, 32, 33, 40, 95, 96, 97, 223, 224, 225, 539, 540, 541, 580, 1400])
