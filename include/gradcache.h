@@ -339,13 +339,17 @@ int gc_dist_dot_block(const void* Q, int64_t ldq, const void* P, int64_t ldp, in
  *   gc_grad_clip    both: *norm = n, *sq_sum = n^2 (sq_sum may be NULL), out = c g.
  *
  * The two calls that write refuse a list in which a place that is written is read or written through another
- * tensor, or through the tensor's own other place (GC_ERR_ALIAS): column ranges of one matrix that do not meet are no
- * such places, matrices of different pitches count as if they were where their first and last bytes enclose one
- * another's.  In place (`out` NULL or equal to `data`, with the same pitch) nothing is written when c = 1.
- * Squares are summed in fp32 over at most 64 values and in fp64 beyond, and in fp64 throughout where they
- * overflow or vanish in fp32: n is off by at most 2^-20 n for any finite values.  c is rounded to fp32,
- * then c g to the tensor's type.  Where n^2 is not finite (a NaN or an infinity among the gradients) *dev_status (may be NULL) gets
- * GC_DEV_GRAD_NONFINITE and c is 1 (so it is for a *sq_sum that is negative): the values stay as they are, or are copied as they are.
+ * tensor, or through the tensor's own other place (GC_ERR_ALIAS).  Column ranges of one matrix that do not meet are no
+ * such places; two matrices of different pitches are taken to share one as soon as one starts between the other's
+ * first and last byte.  In place (`out` NULL or equal to `data`, with the same pitch) nothing is written when c = 1.
+ * norm, sq_sum, the workspace and dev_status lie outside the list's tensors.
+ * Squares are summed in fp32 over at most 32 values and in fp64 beyond, and in fp64 throughout where they
+ * overflow or vanish in fp32: *sq_sum is off by at most 2^-20 of itself for any finite values (a double for its range;
+ * it does not have a double's precision), and *norm by 2^-20 n where n is a normal fp32 number.  For an n above
+ * those *norm is infinite, without a flag, while *sq_sum holds and c is formed from it.  c is rounded to fp32, c g
+ * to fp32 and from there to the tensor's type.  Where n^2 is not finite (a NaN or an infinity among the gradients)
+ * *dev_status (may be NULL) gets GC_DEV_GRAD_NONFINITE and c is 1 (so it is for a *sq_sum that is negative): the values
+ * stay as they are, or are copied as they are.  (torch.nn.utils.clip_grad_norm_ scales them by 0 or NaN.)
  * max_norm >= 0 (an infinity never scales); NaN or negative: GC_ERR_SHAPE.
  * Workspace: gc_grad_workspace_bytes(n_tensors), 256-byte aligned, 0 for invalid arguments; calls that may
  * overlap on the GPU need one each.  Asynchronous on cuda_stream, deterministic.

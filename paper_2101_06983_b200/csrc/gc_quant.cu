@@ -8,7 +8,10 @@
 // gc_matmul_i8 runs on the tensor cores (tcgen05, kind::i8: exact products and 32-bit integer sums).  Long contractions
 // are bound by the products (16384 x 768 x 4096 37 us, 2.8 POP/s; 8192 x 8192 x 4096 163 us, 3.4), short ones by the stores of the
 // result (4096 x 8192 x 768 to fp32 31 us, of which 134 MB take 20.5; to bf16 24), few rows of A by reading B (1 x 131072 x 768 18.7 us,
-// 5.4 TB/s).
+// 5.4 TB/s).  These are times of a call in a graph; called back to back the first is 44 us and the fp32 one 38, since the clock
+// falls under the power limit.  Short contractions with bf16 outputs stay farther from their floors (8192 x 768 x 768
+// 7.7 us against 3.0, 60000 x 768 x 768 32.4 against 21.8), and so do few tiles of long ones (500 x 500 x 8192 11.4 against
+// 1.4: clusters share contractions of up to 64 rows only).
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -839,7 +842,8 @@ struct ImPlan { bool pair, staged; int bn; };
 // The tile that costs least by a count of cycles: rounds of tiles, each its products or loads, whichever is longer, or
 // its stores where they are longer still, and the stores of the last one.  The constants are fitted to 72 shapes with every
 // choice forced, one row to 60000 and contractions of 40 to 8192: 2 % behind the best choice on average, 10 % at
-// most.  bf16 outputs without staging would be 13 % behind (87 % at most), all of them staged 5 (49).
+// most, in times that repeat within a few per cent, long products under the power limit within 20.  bf16 outputs
+// without staging would be 13 % behind (87 % at most), all of them staged 5 (49).
 ImPlan make_im_plan(int64_t rows, int64_t cols, int64_t k, bool bf16) {
     ImPlan best{false, false, 16};
     double least = INFINITY;

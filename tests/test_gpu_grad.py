@@ -1,7 +1,7 @@
 """gc_grad_norm, gc_grad_scale and gc_grad_clip against the definition in 64 bits.
 
-Tolerances.  The norm: at most 64 squares are summed in fp32, in four chains of 16 fused multiply-adds that two
-further additions join, 18 roundings of at most 2^-24 each; everything beyond is fp64, the square root halves
+Tolerances.  The norm: at most 32 squares are summed in fp32, in four chains of 8 fused multiply-adds that two
+further additions join, 10 roundings of at most 2^-24 each; everything beyond is fp64, the square root halves
 the relative error and rounding the result adds 2^-24: below 2^-20.  The scaled values are compared with what
 the returned sum of squares gives: its square root, the division and the rounding to fp32 are IEEE operations, the
 product is rounded once, so they are equal bit for bit."""
