@@ -245,6 +245,18 @@ def test_magnitudes(binding, dtype, size):
     assert abs(both.get_norm() - want) <= 2 * TOL_NORM * want
 
 
+def test_a_norm_beyond_a_float(binding):
+    """Finite gradients whose norm is none: the float is infinite, the sum of squares holds, no flag, and they are scaled."""
+    x = torch.tensor([3e38, -3e38], device="cuda")
+    before = x.clone()
+    call = Call(binding, [x])
+    want = _sum64([x])
+    sq = call.clip(1e30)
+    assert abs(sq - want) <= 2 * TOL_NORM * want
+    assert math.isinf(call.norm.item()) and call.st.item() == 0
+    assert torch.equal(x.cpu(), _scaled(before, _factor(sq, 1e30)))
+
+
 def test_a_tensor_listed_twice(binding):
     """The norm counts it twice; it is scaled into two outputs, but not where it lies."""
     x = torch.randn(70001, device="cuda")
